@@ -288,6 +288,119 @@ int sdlm_profile(sdlm_ctx *ctx, int32_t mask);
 int sdlm_profile_every(sdlm_ctx *ctx, int32_t n);
 int sdlm_profile_read(sdlm_ctx *ctx, float *ms, int32_t *launches);
 
+/*
+ * ---------------------------------------------------------------- Operators on the caller's tensors
+ *
+ * The same kernels that a context runs on its own state, for programs that keep logits or a cache of their own (or want to work on a
+ * context's cache: sdlm_kv_describe).  They take the stream (a hipStream_t; NULL: the default stream) of the device that is current and
+ * holds the tensors, allocate nothing, do not synchronise and keep nothing between calls; two calls may run at once if they share no workspace
+ * and no output, and each may be captured into a graph.  Return value: 0 or a negative sdlm_status, whose text sdlm_op_error() gives.
+ */
+
+/* Text of the last operator call of this thread that failed ([host] string). */
+const char *sdlm_op_error(void);
+
+/*
+ * Draw one token from each row of logits.
+ *
+ * The tokens of a row are ordered by logit, equal logits by index (lowest first); NaN counts as -infinity, and tokens at -infinity are never drawn.  With
+ * w = exp((z - max z) / temperature) a token is kept while
+ *   - it is among the first top_k (top_k <= 0: all), and
+ *   - the weight of those before it, as a share of the first top_k together, is below top_p (top_p >= 1 or NaN: all), and
+ *   - w >= min_p (min_p <= 0 or NaN: all);
+ * the first is always kept.  Drawn is the first kept token, in that order, whose running weight exceeds u times the weight of all kept ones.  A temperature <= 0 (or NaN)
+ * draws the first.  Where the largest logit is +infinity, only the tokens with it have weight.  A row without any token above -infinity gives id -1 and probability 0.
+ * Weights are held to 2^-45 of the largest, in integers: a result does not depend on the launch or on the row's neighbours.  A token whose weight is below that is not drawn.
+ */
+typedef struct {
+    const void *logits;        /* [dev] rows x vocab, element type `dtype` */
+    int64_t row_stride;        /* elements between rows, >= vocab */
+    int32_t dtype;             /* 0: fp32, 1: bf16 */
+    int32_t rows, vocab;       /* rows >= 0; vocab 1 .. 524288 */
+    const float *temperature;  /* [dev, rows] or NULL: 1 */
+    const int32_t *top_k;      /* [dev, rows] or NULL: off */
+    const float *top_p, *min_p;/* [dev, rows] or NULL: off */
+    const float *u;            /* [dev, rows] uniform numbers in [0, 1); others are clamped */
+    int32_t *ids;              /* [dev, rows] drawn tokens */
+    float *prob;               /* [dev, rows] their share of the kept weight, or NULL */
+} sdlm_sample_args;
+size_t sdlm_sample_workspace_bytes(int32_t rows, int32_t vocab);   /* 0 for sizes outside the limits */
+/* workspace [dev]: 256-byte aligned.  Errors: SDLM_EINVAL, SDLM_ECAPACITY (workspace too small), SDLM_EHIP. */
+int sdlm_sample(const sdlm_sample_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * A paged K/V cache.  `pool` holds tiles of 16 positions of one (layer, kv head): layer l, tile t, kv head h starts at element
+ * l * layer_stride + (t * n_kv_heads + h) * 32 * head_dim.  Inside, first K, element i of slot s at (i / 8) * 128 + s * 8 + i % 8; then,
+ * from 16 * head_dim on, V at ((i / 16) * 4 + s / 4) * 64 + (i % 16) * 4 + s % 4.  Position p of sequence b is slot p % 16 of tile
+ * page_table[b * pages_per_seq + p / 16], in every layer and head.  Tiles 0 .. n_pages-1 are the pages that sequences can hold; a pool may have more tiles, for
+ * other uses.  All pointers [dev]; a call reads and writes what its text names, and entries outside their range are never followed.
+ */
+typedef struct {
+    void *pool;                /* 16-byte aligned */
+    int64_t layer_stride;      /* elements between layers, a multiple of 8 (fp32: 4) */
+    int32_t n_layers, n_tiles; /* n_tiles: tiles in a layer */
+    int32_t n_kv_heads, head_dim;   /* head_dim 32, 64, 96 or 128 */
+    int32_t dtype;             /* 0: fp32, 1: bf16 */
+    int32_t n_pages;
+    int32_t max_seqs, pages_per_seq;
+    int32_t *page_table;       /* max_seqs x pages_per_seq; -1: no page */
+    int32_t *lengths;          /* max_seqs: positions that hold K/V */
+    int32_t *backed;           /* max_seqs: pages that the sequence holds */
+    int32_t *page_refs;        /* n_pages: sequences that hold the page (0: free) */
+    int32_t *free_pages;       /* n_pages: the free pages in ascending order, then -1 */
+    int32_t *free_count;       /* 1 */
+} sdlm_kv;
+
+/*
+ * Attention of a tree of drafted tokens for each of n_seqs sequences over the cache.  Rows node_offsets[b] .. node_offsets[b+1]-1 of q and out are the nodes of sequence b
+ * (at most max_nodes; further rows are left alone).  Node i of b sees the positions 0 .. lengths[b]-1 of the cache and those nodes j of b whose bit (word j / 64, bit j % 64) is set in row
+ * node_offsets[b] + i of `mask`; a tree of drafts sets the node's own bit and its ancestors', but any mask will do.  K/V of node j are at position node_base[b] + j
+ * of the table node_table (n_seqs x node_pages entries): the sequence's own table with node_base = lengths, where nodes are appended behind the cache, or pages of their own.
+ *   out[r, h] = sum_j softmax_j(q[r, h] . K[j] / sqrt(head_dim)) V[j]; zeros for a node that sees nothing.
+ * Query head h reads kv head h / (n_q_heads / n_kv_heads).  bf16: the softmax's weights are rounded to bf16 in front of the product with V (half a step of 2^-8 each, as in a context's own
+ * attention); sums, maxima and the division are fp32.  K/V that a node does not see may hold anything, NaN too, and changes nothing.  Reads pool, page_table and lengths of `kv`.
+ */
+typedef struct {
+    const void *q;               /* [dev] n_rows x n_q_heads x head_dim, element type of the cache */
+    void *out;                   /* [dev] as q; must not overlap it */
+    int64_t q_stride, out_stride;/* elements between rows, >= n_q_heads * head_dim, multiples of 16 bytes; both base pointers 16-byte aligned */
+    int32_t n_rows, n_seqs;      /* n_rows: rows of q and out in all; n_seqs <= kv->max_seqs */
+    int32_t n_q_heads;           /* a multiple of n_kv_heads */
+    int32_t max_nodes;           /* 1 .. 1024: most nodes of a sequence */
+    int32_t max_len;             /* most positions of the cache a sequence has; 0: what the table can hold.  Steers the launch; longer ones are still read whole */
+    const int32_t *node_offsets; /* [dev, n_seqs + 1] ascending, 0 .. n_rows */
+    const int64_t *mask;         /* [dev] n_rows x mask_words */
+    int32_t mask_words;          /* >= (max_nodes + 63) / 64 */
+    int32_t node_pages;          /* entries of node_table a sequence */
+    const int32_t *node_table;   /* [dev] */
+    const int32_t *node_base;    /* [dev, n_seqs] or NULL: 0 */
+} sdlm_tree_args;
+size_t sdlm_tree_attention_workspace_bytes(const sdlm_kv *kv, int32_t n_q_heads, int32_t n_seqs, int32_t max_nodes, int32_t max_len);
+int sdlm_tree_attention(const sdlm_kv *kv, int32_t layer, const sdlm_tree_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Make n_new sequences out of the cache's present ones: sequence b becomes what sequence parent[b] is now (-1: an empty one), and sequences from n_new on become empty.  A parent may be
+ * named many times (samples of one prompt, a beam's survivors) or not at all, which frees it.
+ *   share != 0: the first lengths / 16 pages, which are full, are held in common; the others (the one that is being written, and pages backed ahead) are each sequence's own.
+ *   share == 0: all pages are.
+ * Own pages stay with a sequence that is its own parent, or else with the first that has it as its parent; the others take free pages, the lowest first, in the
+ * order of sequences and positions, with the contents copied where a page has positions below lengths.  Pages that nobody holds any more are free at once, for this call too.
+ * A sequence must not write to positions below the length that it was forked with, and its length must not fall below that while it shares pages.
+ * Updates page_table, lengths, backed, page_refs (counted anew from the tables), free_pages, free_count and the copied tiles of `pool`.
+ *   status [dev, 1]: 0, or nothing was changed: bit 0: there are not enough free pages; bit 1: a parent, or a page in the table, is out of range.
+ */
+size_t sdlm_kv_fork_workspace_bytes(const sdlm_kv *kv);
+int sdlm_kv_fork(const sdlm_kv *kv, const int32_t *parent, int32_t n_new, int32_t share, int32_t *status, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Move the K/V of accepted tree nodes into the cache, in every layer: node path[b * path_stride + i] of sequence b to position lengths[b] + i, for i < path_len[b] (at most max_path).
+ * Nodes are found as in sdlm_tree_attention.  A path has to ascend.  The destination's pages must be in the table, and not shared.  Nodes or positions without a page
+ * are passed over.  lengths is left as it is: the caller adds path_len when it publishes the tokens, and until then the call may be repeated, unless the nodes stand
+ * behind the sequence in its own pages, where it overwrites them.
+ */
+int sdlm_kv_compact(const sdlm_kv *kv, int32_t n_seqs, const int32_t *path, int32_t path_stride, const int32_t *path_len, int32_t max_path, const int32_t *node_table,
+                    int32_t node_pages, const int32_t *node_base, void *hip_stream);
+
 /* Which kernel family serves the GEMMs and the attention: "generic-fp32", "mfma-bf16", ... ([host] string). */
 const char *sdlm_kernel_info(const sdlm_ctx *ctx);
 

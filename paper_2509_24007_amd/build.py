@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsdlm.so")
-SOURCES = ["sdlm_api.hip", "kernels_generic.hip", "kernels_mfma.hip", "attn_mfma.hip"]
+SOURCES = ["sdlm_api.hip", "kernels_generic.hip", "kernels_mfma.hip", "attn_mfma.hip", "ops_api.hip", "sample.hip", "tree_attn.hip", "kv_pages.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -43,7 +43,7 @@ def build(force: bool = False, verbose: bool = True) -> str:
         if verbose and out.strip():
             print(out)
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         list(ex.map(run, jobs))
     objs = [os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES]
     if force or jobs or not os.path.exists(LIB):

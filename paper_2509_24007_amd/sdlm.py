@@ -23,7 +23,8 @@ STEP_PLAN = ("chain", "embeds", "qkv_rows", "qkv_rest", "lm_head", "lm_accept", 
 EXPORTS = ("sdlm_workspace_bytes", "sdlm_create", "sdlm_init_weights", "sdlm_prefill", "sdlm_decode_step",
            "sdlm_decode_step_static", "sdlm_graph", "sdlm_verify_step", "sdlm_kv_commit", "sdlm_get_lengths", "sdlm_debug_tap", "sdlm_debug_rows", "sdlm_debug_read_kv",
            "sdlm_debug_gemm_plan", "sdlm_debug_step_plan", "sdlm_max_rows", "sdlm_profile", "sdlm_profile_every", "sdlm_profile_read", "sdlm_kernel_info", "sdlm_last_error",
-           "sdlm_destroy")
+           "sdlm_destroy", "sdlm_op_error", "sdlm_sample_workspace_bytes", "sdlm_sample", "sdlm_tree_attention_workspace_bytes", "sdlm_tree_attention",
+           "sdlm_kv_fork_workspace_bytes", "sdlm_kv_fork", "sdlm_kv_compact")
 
 
 class ModelCfg(C.Structure):
@@ -48,6 +49,25 @@ class Weights(C.Structure):
     _fields_ = [("embed", C.c_void_p), ("lm_head", C.c_void_p), ("final_norm", C.c_void_p),
                 ("attn_norm", _PP), ("wq", _PP), ("wk", _PP), ("wv", _PP), ("wo", _PP),
                 ("bq", _PP), ("bk", _PP), ("bv", _PP), ("ffn_norm", _PP), ("w_gate", _PP), ("w_up", _PP), ("w_down", _PP)]
+
+
+class SampleArgs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("row_stride", C.c_int64), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32),
+                ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("u", C.c_void_p),
+                ("ids", C.c_void_p), ("prob", C.c_void_p)]
+
+
+class KvDesc(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("layer_stride", C.c_int64), ("n_layers", C.c_int32), ("n_tiles", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("n_pages", C.c_int32), ("max_seqs", C.c_int32), ("pages_per_seq", C.c_int32),
+                ("page_table", C.c_void_p), ("lengths", C.c_void_p), ("backed", C.c_void_p), ("page_refs", C.c_void_p), ("free_pages", C.c_void_p),
+                ("free_count", C.c_void_p)]
+
+
+class TreeArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64), ("n_rows", C.c_int32), ("n_seqs", C.c_int32),
+                ("n_q_heads", C.c_int32), ("max_nodes", C.c_int32), ("max_len", C.c_int32), ("node_offsets", C.c_void_p), ("mask", C.c_void_p),
+                ("mask_words", C.c_int32), ("node_pages", C.c_int32), ("node_table", C.c_void_p), ("node_base", C.c_void_p)]
 
 
 _lib = None
@@ -106,6 +126,22 @@ def load():
     L.sdlm_last_error.argtypes = [vp]
     L.sdlm_destroy.restype = None
     L.sdlm_destroy.argtypes = [vp]
+    L.sdlm_op_error.restype = C.c_char_p
+    L.sdlm_op_error.argtypes = []
+    L.sdlm_sample_workspace_bytes.restype = sz
+    L.sdlm_sample_workspace_bytes.argtypes = [i32, i32]
+    L.sdlm_sample.restype = C.c_int
+    L.sdlm_sample.argtypes = [vp, vp, sz, vp]
+    L.sdlm_tree_attention_workspace_bytes.restype = sz
+    L.sdlm_tree_attention_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    L.sdlm_tree_attention.restype = C.c_int
+    L.sdlm_tree_attention.argtypes = [vp, i32, vp, vp, sz, vp]
+    L.sdlm_kv_fork_workspace_bytes.restype = sz
+    L.sdlm_kv_fork_workspace_bytes.argtypes = [vp]
+    L.sdlm_kv_fork.restype = C.c_int
+    L.sdlm_kv_fork.argtypes = [vp, vp, i32, i32, vp, vp, sz, vp]
+    L.sdlm_kv_compact.restype = C.c_int
+    L.sdlm_kv_compact.argtypes = [vp, i32, vp, i32, vp, i32, vp, i32, vp, vp]
     _lib = L
     return L
 
@@ -341,3 +377,130 @@ class Context:
         cnt = (C.c_int32 * len(PHASES))()
         self._check(self.L.sdlm_profile_read(self.h, ms, cnt))
         return {p: (float(ms[i]), int(cnt[i])) for i, p in enumerate(PHASES)}
+
+
+# ---------------------------------------------------------------- operators on the caller's tensors
+
+PAGE = 16
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _need(ok: bool, msg: str) -> None:
+    if not ok:
+        raise SdlmError(EINVAL, msg)
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str, dev, dtype=torch.int32) -> Optional[int]:
+    """Address of a contiguous vector of at least n entries on the operator's device."""
+    if t is None:
+        return None
+    _need(t.dtype == dtype and t.device == dev and t.is_contiguous() and t.numel() >= n, f"{name} must be {n} or more contiguous {dtype} on {dev}")
+    return t.data_ptr()
+
+
+def _run_op(dev, fn, *args) -> None:
+    """Call an entry point on the tensors' device and that device's current stream."""
+    if dev.index == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if rc != 0:
+        raise SdlmError(rc, load().sdlm_op_error().decode())
+
+
+def _scratch(need: int, dev) -> torch.Tensor:
+    if need == 0:
+        raise SdlmError(EINVAL, load().sdlm_op_error().decode() or "sizes outside the operator's limits")
+    return torch.empty(need, dtype=torch.uint8, device=dev)
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None):
+    """Draw one token from each row of logits [rows, vocab] (fp32 or bf16, the last dimension contiguous) with the uniform numbers u [rows]; the settings are
+    vectors over the rows or None (see sdlm_sample in the header).  Returns ids [rows] int32 and their probabilities [rows] fp32.  Runs on the current stream."""
+    L = load()
+    _need(logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be [rows, vocab] fp32 or bf16 on a GPU, the last dimension contiguous")
+    R, V = logits.shape
+    dev, f32 = logits.device, torch.float32
+    stride = logits.stride(0) if R > 1 else V
+    ids = torch.empty(R, dtype=torch.int32, device=dev)
+    prob = torch.empty(R, dtype=f32, device=dev)
+    a = SampleArgs(logits.data_ptr(), stride, _DTYPES[logits.dtype], R, V, _ints(temperature, R, "temperature", dev, f32), _ints(top_k, R, "top_k", dev),
+                   _ints(top_p, R, "top_p", dev, f32), _ints(min_p, R, "min_p", dev, f32), _ints(u, R, "u", dev, f32), ids.data_ptr(), prob.data_ptr())
+    if R:
+        need = L.sdlm_sample_workspace_bytes(R, V)
+        _need(need > 0, f"{R} rows of {V} logits are outside the limits")
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        _run_op(dev, L.sdlm_sample, C.byref(a), ws.data_ptr(), need)
+    return ids, prob
+
+
+class KvCache:
+    """A paged K/V cache in the caller's tensors (sdlm_kv in the header): pool [layers, tiles, kv heads, 2, 16 * head_dim] fp32 or bf16, page_table [sequences,
+    pages a sequence], lengths [sequences].  Forking needs the rest: n_pages, backed [sequences], page_refs [n_pages], free_pages [n_pages] and free_count [1].  All
+    int32 on the pool's device.  The operators run on that device's current stream."""
+
+    def __init__(self, pool: torch.Tensor, *, page_table: torch.Tensor, lengths: torch.Tensor, n_pages: int = 0, backed: Optional[torch.Tensor] = None,
+                 page_refs: Optional[torch.Tensor] = None, free_pages: Optional[torch.Tensor] = None, free_count: Optional[torch.Tensor] = None):
+        _need(pool.is_cuda and pool.dim() == 5 and pool.dtype in _DTYPES and pool.shape[3] == 2 and pool.shape[4] % PAGE == 0, "pool must be [layers, tiles, kv heads, 2, 16 * head_dim] fp32 or bf16 on a GPU")
+        _need(pool[0].is_contiguous(), "a layer of the pool must be contiguous")
+        _need(page_table.dim() == 2, "page_table must be [sequences, pages a sequence]")
+        self.device = dev = pool.device
+        self.dtype, self.head_dim, self.n_kv_heads = pool.dtype, pool.shape[4] // PAGE, pool.shape[2]
+        S, pps = page_table.shape
+        stride = pool.stride(0) if pool.shape[0] > 1 else pool[0].numel()
+        self._keep = (pool, page_table, lengths, backed, page_refs, free_pages, free_count)
+        self.max_seqs, self.pages_per_seq = S, pps
+        self.desc = KvDesc(pool.data_ptr(), stride, pool.shape[0], pool.shape[1], pool.shape[2], self.head_dim, _DTYPES[pool.dtype], n_pages, S, pps,
+                           _ints(page_table, S * pps, "page_table", dev), _ints(lengths, S, "lengths", dev), _ints(backed, S, "backed", dev),
+                           _ints(page_refs, n_pages, "page_refs", dev), _ints(free_pages, n_pages, "free_pages", dev), _ints(free_count, 1, "free_count", dev))
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+
+    def fork(self, parent: torch.Tensor, *, share: bool = True) -> None:
+        """Sequence b becomes what sequence parent[b] is (-1: empty); see sdlm_kv_fork.  Does not synchronise: check() raises if the last fork was refused."""
+        L = load()
+        need = L.sdlm_kv_fork_workspace_bytes(C.byref(self.desc))
+        ws = _scratch(need, self.device)
+        _run_op(self.device, L.sdlm_kv_fork, C.byref(self.desc), _ints(parent, 0, "parent", self.device), parent.numel(), int(share), self.status.data_ptr(), ws.data_ptr(), need)
+
+    def check(self) -> None:
+        """Synchronise and raise if the last fork was refused."""
+        bad = int(self.status.item())
+        if bad & 2:
+            raise SdlmError(EINVAL, "a parent or a page of the table is out of range: nothing was changed")
+        if bad:
+            raise SdlmError(ECAPACITY, "not enough free pages: nothing was changed")
+
+    def compact(self, path: torch.Tensor, path_len: torch.Tensor, *, node_table: torch.Tensor, node_base: Optional[torch.Tensor] = None) -> None:
+        """Move the K/V of nodes path[b, :path_len[b]] to the positions from lengths[b] on, in every layer; see sdlm_kv_compact."""
+        dev = self.device
+        _need(path.dim() == 2 and node_table.dim() == 2 and node_table.shape[0] >= path.shape[0], "path must be [sequences, most nodes], node_table [sequences, pages]")
+        S, P = path.shape
+        _run_op(dev, load().sdlm_kv_compact, C.byref(self.desc), S, _ints(path, S * P, "path", dev), P, _ints(path_len, S, "path_len", dev), P,
+                _ints(node_table, 1, "node_table", dev), node_table.shape[1], _ints(node_base, S, "node_base", dev))
+
+
+def tree_attention(kv: KvCache, layer: int, q: torch.Tensor, node_offsets: torch.Tensor, mask: torch.Tensor, *, node_table: torch.Tensor, max_nodes: int,
+                   node_base: Optional[torch.Tensor] = None, max_len: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of drafted token trees over one layer of the cache (see sdlm_tree_attention): q [nodes, query heads, head_dim] of the cache's type, rows node_offsets[b] up to
+    node_offsets[b + 1] belong to sequence b; mask [nodes, words] int64, bit j of a row: the node sees node j of its sequence.  Returns out, shaped as q."""
+    L, dev = load(), kv.device
+    _need(q.dim() == 3 and q.shape[2] == kv.head_dim and q.dtype == kv.dtype and q.device == dev, "q must be [nodes, query heads, head_dim] of the cache's type and device")
+    _need(mask.dim() == 2 and node_table.dim() == 2, "mask must be [nodes, words], node_table [sequences, pages]")
+    N, H, d = q.shape
+    S = node_offsets.numel() - 1
+    if out is None:
+        out = torch.empty(N, H, d, dtype=q.dtype, device=dev)
+    _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev, "out must be shaped as q, of its type and device")
+    for t in (q, out):
+        _need(t.stride(2) == 1 and (t.stride(1) == d or H == 1), "the heads of a row of q and out must be contiguous")
+    _need(S >= 0 and node_table.shape[0] >= S and mask.shape[0] >= N, "node_offsets, node_table and mask must agree with the nodes")
+    row = H * d
+    a = TreeArgs(q.data_ptr(), out.data_ptr(), q.stride(0) if N > 1 else row, out.stride(0) if N > 1 else row, N, S, H, max_nodes, max_len,
+                 _ints(node_offsets, S + 1, "node_offsets", dev), _ints(mask, N, "mask", dev, torch.int64), mask.shape[1], node_table.shape[1],
+                 _ints(node_table, 1, "node_table", dev), _ints(node_base, S, "node_base", dev))
+    need = L.sdlm_tree_attention_workspace_bytes(C.byref(kv.desc), H, S, max_nodes, max_len)
+    ws = _scratch(need, dev)
+    _run_op(dev, L.sdlm_tree_attention, C.byref(kv.desc), layer, C.byref(a), ws.data_ptr(), need)
+    return out

@@ -1,0 +1,574 @@
+"""The operators on the caller's tensors against plain 64-bit implementations of their definitions."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import operators_plain as plain
+from paper_2509_24007_amd import sdlm
+
+pytestmark = pytest.mark.gpu
+
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def dev(a, dtype=torch.int32):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(dtype).cuda()
+
+
+# ---------------------------------------------------------------------------------------------------------------- sampling
+
+def check_sample(logits, t, k, p, m, u):
+    """ids equal, probabilities within the two roundings (the weight's 2^-45 of the largest is below them, and one to fp32): 2^-23 relative."""
+    R = logits.shape[0]
+    f = torch.float32
+    t, p, m, u = [np.broadcast_to(np.asarray(v, np.float32), (R,)) for v in (t, p, m, u)]
+    k = np.broadcast_to(np.asarray(k, np.int32), (R,))
+    ids, prob = sdlm.sample(logits, dev(u, f), temperature=dev(t, f), top_k=dev(k), top_p=dev(p, f), min_p=dev(m, f))
+    z = logits.double().cpu().numpy()
+    want = [plain.sample_row(z[r], float(t[r]), int(k[r]), float(p[r]), float(m[r]), float(u[r])) for r in range(R)]
+    assert ids.cpu().tolist() == [w[0] for w in want]
+    np.testing.assert_allclose(prob.double().cpu().numpy(), [w[1] for w in want], rtol=2.0 ** -23, atol=2.0 ** -44)
+
+
+def draw_logits(seed, R, V, dtype, spread=1.6, pad=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = torch.empty(R, V + pad, device="cuda").exponential_(1.0, generator=g) * spread
+    return z.to(DT[dtype])[:, :V], np.random.default_rng(seed)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("R,V,pad", [(1, 1, 0), (3, 2, 5), (5, 63, 0), (4, 64, 1), (7, 65, 3), (6, 257, 0), (9, 1000, 8), (8, 4096, 0), (5, 4097, 1), (3, 33003, 29), (4, 152064, 0), (2, 262144, 0), (1, 524288, 0)])
+def test_sample_sizes(dtype, R, V, pad):
+    z, rng = draw_logits(R * 1000 + V, R, V, dtype, pad=pad)
+    for _ in range(3):
+        check_sample(z, rng.choice([0.0, 0.3, 0.7, 1.0, 1.5], R), rng.choice([0, 1, 5, 50, 1000], R), rng.choice([1.0, 0.1, 0.5, 0.9, 0.99], R), rng.choice([0.0, 0.05, 0.3], R), rng.random(R))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("t,k,p,m", [(1.0, 0, 1.0, 0.0), (1.0, 0, 0.95, 0.0), (2.0, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.02), (1.0, 1000, 1.0, 0.0), (1.0, 5000, 0.99, 0.0), (0.2, 0, 1.0, 0.0), (5.0, 0, 1.0, 0.0),
+                                     (1.0, 1, 0.5, 0.5), (0.0, 40, 0.9, 0.1), (-1.0, 0, 1.0, 0.0), (1.0, 30, 0.0, 0.0), (1.0, 0, 1.0, 1.0), (1.0, 0, 1.0, 3.0), (1e-3, 0, 1.0, 0.0),
+                                     (1e-30, 0, 0.9, 0.0), (1e30, 0, 0.9, 0.0), (1.0, 10 ** 9, 2.0, -1.0), (float("nan"), 0, 0.9, 0.0), (1.0, 0, float("nan"), float("nan"))])
+def test_sample_settings(dtype, t, k, p, m):
+    z, rng = draw_logits(17, 6, 20011, dtype, spread=1.3)
+    check_sample(z, t, k, p, m, [0.0, 0.13, 0.5, 0.77, 0.999, float(np.float32(1) - np.float32(2.0 ** -24))])
+
+
+def test_sample_whole_distribution():
+    """Every token is drawn by the numbers of its own interval: 64 evenly spaced u over 64 equal tokens, then over unequal ones."""
+    V = 64
+    z = torch.zeros(V, V, device="cuda")
+    u = torch.arange(V, device="cuda").float() / V + 0.5 / V
+    ids, prob = sdlm.sample(z, u)
+    assert ids.cpu().tolist() == list(range(V)) and torch.equal(prob.cpu(), torch.full((V,), 1.0 / V))
+    check_sample(torch.linspace(-3, 3, V, device="cuda").repeat(V, 1).contiguous(), 1.0, 0, 1.0, 0.0, u.cpu().numpy())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("values", [1, 2, 7, 300])
+def test_sample_ties(dtype, values):
+    """Few different values: the lowest index wins each bound that falls among equal logits, however many there are."""
+    rng = np.random.default_rng(values)
+    z = dev(rng.integers(0, values, (6, 50021)) * 0.25, DT[dtype])
+    for k, p in [(0, 1.0), (1, 1.0), (777, 1.0), (49999, 1.0), (0, 0.3), (0, 0.999), (20000, 0.5)]:
+        check_sample(z, 1.0, k, p, 0.0, rng.random(6))
+
+
+def test_sample_masks_and_non_finite():
+    V, inf, nan = 5003, math.inf, math.nan
+    z = torch.randn(10, V, generator=torch.Generator().manual_seed(3))
+    z[0] = -inf
+    z[1] = nan
+    z[2, :-1] = -inf                                # one token left, the last
+    z[3, ::2] = nan
+    z[4, 100] = inf
+    z[5, 7], z[5, 4000] = inf, inf
+    z[6] = torch.finfo(torch.float32).min           # a mask that wrote the type's lowest value everywhere
+    z[7, 1:] = torch.finfo(torch.float32).min
+    z[8, :] = 0.0
+    z[8, ::3] = -0.0                                # equal to 0: ordered by index
+    z[9, 50:] = -inf
+    z = z.cuda()
+    rng = np.random.default_rng(5)
+    for k, p, m in [(0, 1.0, 0.0), (3, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.1), (100, 0.5, 0.01)]:
+        for t in (0.0, 0.7):
+            check_sample(z, t, k, p, m, rng.random(10))
+
+
+def test_sample_uniform_out_of_range_and_defaults():
+    z, _ = draw_logits(2, 4, 999, "fp32")
+    check_sample(z, 1.0, 0, 1.0, 0.0, [-1.0, 1.0, 7.0, 0.25])
+    u = torch.rand(4, device="cuda")
+    a, b = sdlm.sample(z, u), sdlm.sample(z, u, temperature=torch.ones(4, device="cuda"), top_k=torch.zeros(4, dtype=torch.int32, device="cuda"))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    ids, prob = sdlm.sample(z[:0], u[:0])
+    assert ids.numel() == 0 and prob.numel() == 0
+
+
+def test_sample_rows_do_not_depend_on_each_other():
+    z, rng = draw_logits(11, 64, 40009, "fp32")
+    t = dev(rng.choice([0.5, 1.0], 64), torch.float32)
+    u, p = dev(rng.random(64), torch.float32), dev(rng.choice([0.8, 1.0], 64), torch.float32)
+    ids, prob = sdlm.sample(z, u, temperature=t, top_p=p)
+    for r in (0, 5, 63):
+        i1, p1 = sdlm.sample(z[r:r + 1], u[r:r + 1], temperature=t[r:r + 1], top_p=p[r:r + 1])
+        assert i1.item() == ids[r].item() and p1.item() == prob[r].item()
+
+
+# ---------------------------------------------------------------------------------------------------------------- tree attention
+
+def tree_case(seed, heads, lens, nodes, dtype, inplace=False, kind="tree", junk=False):
+    """A cache with scattered pages; kind: tree (ancestors), full, self, empty (every third row sees no node) or random masks."""
+    hq, hkv, d = heads
+    rng = np.random.default_rng(seed)
+    B, mx = len(lens), max(nodes)
+    pps = max(1, -(-(max(lens) + (mx if inplace else 0)) // 16)) + 1
+    npp = -(-mx // 16) + 1
+    order = rng.permutation(B * (pps + npp))
+    table, ntab = order[:B * pps].reshape(B, pps), order[B * pps:].reshape(B, npp)
+    g = torch.Generator().manual_seed(seed)
+    pool = torch.randn(1, B * (pps + npp), hkv, 2, 16 * d, generator=g).to(DT[dtype])
+    offs = np.concatenate([[0], np.cumsum(nodes)])
+    seen = np.zeros((offs[-1], mx), bool)
+    for b in range(B):
+        for i in range(nodes[b]):
+            row = seen[offs[b] + i]
+            if kind == "tree":
+                par = int(rng.integers(max(-1, i - 5), i)) if i else -1
+                if par >= 0:
+                    row[:] = seen[offs[b] + par]
+                row[i] = True
+            elif kind == "full":
+                row[:nodes[b]] = True
+            elif kind == "self":
+                row[i] = True
+            elif kind == "empty":
+                row[i] = i % 3 != 0
+            else:
+                row[:nodes[b]] = rng.random(nodes[b]) < 0.3
+    words = (mx + 63) // 64
+    bits = np.zeros((offs[-1], words * 64), np.uint8)
+    bits[:, :mx] = seen
+    mask = np.packbits(bits, axis=1, bitorder="little").view(np.int64)
+    q = (torch.randn(offs[-1], hq, d, generator=g) * 1.5).to(DT[dtype])
+    base = np.array(lens) if inplace else np.zeros(B, int)
+    if inplace:
+        ntab = table
+    if junk:      # what no node sees holds NaN: slots behind the nodes, behind the prefix, and whole tiles of no sequence
+        used = np.zeros((pool.shape[1], 16), bool)
+        for b in range(B):
+            for pos in range(lens[b]):
+                used[table[b][pos // 16], pos % 16] = True
+            for j in np.flatnonzero(seen[offs[b]:offs[b + 1]].any(0)):
+                used[ntab[b][(base[b] + j) // 16], (base[b] + j) % 16] = True
+        i = np.arange(d)
+        for t in range(pool.shape[1]):
+            for s in np.flatnonzero(~used[t]):
+                pool[0, t, :, 0, plain.k_index(s, i)] = math.nan
+                pool[0, t, :, 1, plain.v_index(s, i)] = math.inf
+    return dict(pool=pool, table=table, ntab=ntab, lens=lens, offs=offs, seen=seen, mask=mask, q=q, base=base, nodes=nodes, max_nodes=mx)
+
+
+def run_tree(c, **kw):
+    kv = sdlm.KvCache(c["pool"].cuda(), page_table=dev(c["table"]), lengths=dev(c["lens"]))
+    return sdlm.tree_attention(kv, 0, kw.pop("q", c["q"].cuda()), dev(c["offs"]), torch.from_numpy(c["mask"].copy()).cuda(), node_table=dev(c["ntab"]), node_base=dev(c["base"]),
+                               max_nodes=kw.pop("max_nodes", c["max_nodes"]), **kw)
+
+
+def check_tree(c, out):
+    """bf16: the weights, at most 1, are rounded to half a step of 2^-8 each before they meet V, and so is the result; their sum is not rounded, so the error is at most 2^-8 times the
+    weighted mean of |V| plus 2^-8 of the result, and fp32 sums far below that.  fp32: sums of up to some thousand terms, each product within 2^-24, in an order that halves the error's
+    growth: 2^-24 * 64 of the weighted mean of |V|, and the exponents' error, 2^-24 * |score| with scores up to 32: another 2^-24 * 64."""
+    x = c["pool"][0].double().numpy()
+    ref = plain.tree_attention(x, c["q"].double().numpy(), c["table"], c["lens"], c["offs"], c["seen"], c["ntab"], c["base"])
+    vmean = plain.tree_attention(np.concatenate([x[:, :, :1], np.abs(x[:, :, 1:])], 2), c["q"].double().numpy(), c["table"], c["lens"], c["offs"], c["seen"], c["ntab"], c["base"])
+    got = out.double().cpu().numpy()
+    step = 2.0 ** -8 if c["q"].dtype == torch.bfloat16 else 2.0 ** -24 * 128
+    assert np.isfinite(got).all()
+    worst = np.max(np.abs(got - ref) / (step * vmean + step * np.abs(ref) + 1e-30))
+    assert worst <= 1.0, worst
+
+
+HEADS = [(4, 2, 64), (12, 2, 128), (7, 1, 128), (8, 8, 32), (15, 3, 96)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_tree_attention_heads(heads, dtype):
+    c = tree_case(1, heads, [37, 0, 16, 130, 1], [5, 9, 1, 17, 33], dtype)
+    check_tree(c, run_tree(c))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kind", ["tree", "full", "self", "empty", "random"])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_tree_attention_masks(kind, inplace, dtype):
+    """Masks of every sort over prefixes that end inside a tile or are missing; rows that see nothing are zero."""
+    c = tree_case(2, (4, 2, 64), [21, 0, 0, 64, 15], [20, 7, 70, 16, 3], dtype, inplace=inplace, kind=kind)
+    out = run_tree(c)
+    check_tree(c, out)
+    if kind == "empty":
+        assert (out[c["offs"][1]] == 0).all()      # no prefix, no node
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_tree_attention_ignores_what_is_not_seen(inplace, dtype):
+    for heads in [(4, 2, 64), (14, 2, 128)]:
+        c = tree_case(3, heads, [19, 0, 48, 3], [6, 18, 2, 35], dtype, inplace=inplace, kind="tree", junk=True)
+        x = c["pool"].clone()
+        c["pool"] = torch.nan_to_num(x, nan=0.0, posinf=0.0)
+        ref = run_tree(c)
+        check_tree(c, ref)
+        c["pool"] = x
+        out = run_tree(c)
+        assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("heads,lens,nodes,dtype", [
+    ((12, 2, 128), [512], [12], "bf16"), ((28, 4, 128), [2100, 3, 900], [16, 1, 7], "bf16"), ((16, 2, 128), [4100], [256], "bf16"), ((16, 2, 128), [1, 700], [300, 129], "bf16"),
+    ((40, 8, 128), [5000, 4999], [1, 1], "bf16"), ((8, 8, 64), [1500, 15, 16, 17], [64, 65, 63, 1], "bf16"), ((6, 1, 32), [3000], [128], "bf16"), ((15, 3, 96), [1111, 0], [40, 41], "bf16"),
+    ((4, 2, 64), [2000, 31], [100, 200], "fp32"), ((3, 1, 128), [0, 0, 1], [1, 1, 1], "bf16"), ((64, 1, 64), [333], [5], "bf16"), ((2, 2, 128), [40], [1024], "bf16"), ((16, 2, 128), [6000, 0, 77], [1, 1, 1], "fp32")])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_tree_attention_sizes(heads, lens, nodes, dtype, inplace):
+    c = tree_case(sum(lens) + sum(nodes), heads, lens, nodes, dtype, inplace=inplace)
+    out = run_tree(c)
+    check_tree(c, out)
+    assert torch.equal(out, run_tree(c, max_len=max(1, max(lens))))      # the hint steers the launch only
+
+
+def test_tree_attention_of_one_node_is_a_single_token():
+    """A node that sees itself behind the cache: ordinary decoding of a batch, 70 sequences of 0 to 69 * 7 positions."""
+    c = tree_case(9, (8, 2, 128), [7 * i for i in range(70)], [1] * 70, "bf16", inplace=True)
+    check_tree(c, run_tree(c))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_tree_attention_strides_and_other_rows(dtype):
+    """q inside a wider projection, out inside a wider buffer; rows behind the last sequence and elements between the rows stay as they were."""
+    c = tree_case(4, (6, 2, 64), [40, 9], [5, 11], dtype)
+    N, row = 16, 6 * 64
+    wide = torch.full((N + 3, row + 128), 7.0, dtype=DT[dtype], device="cuda")
+    wide[:N, :row] = c["q"].cuda().view(N, row)
+    q = wide[:, :row].unflatten(1, (6, 64))
+    buf = torch.full((N + 3, row + 64), -3.0, dtype=DT[dtype], device="cuda")
+    mask = np.concatenate([c["mask"], np.full((3, c["mask"].shape[1]), -1)])
+    c2 = dict(c, mask=mask)
+    out = run_tree(c2, q=q, out=buf[:, :row].unflatten(1, (6, 64)), max_nodes=16)
+    check_tree(c, out[:N])
+    assert (buf[N:] == -3).all() and (buf[:, row:] == -3).all()
+
+
+def test_tree_attention_ends_at_max_nodes():
+    """More rows than max_nodes between two offsets: those beyond are not computed, and nothing is written for them."""
+    c = tree_case(5, (4, 2, 64), [40], [20], "bf16", kind="self")
+    out = torch.full((20, 4, 64), -3.0, dtype=torch.bfloat16, device="cuda")
+    kv = sdlm.KvCache(c["pool"].cuda(), page_table=dev([c["table"][0], c["table"][0]]), lengths=dev([40, 0]))
+    sdlm.tree_attention(kv, 0, c["q"].cuda(), dev([0, 20, 20]), torch.from_numpy(c["mask"].copy()).cuda(), node_table=dev([c["ntab"][0], c["ntab"][0]]), max_nodes=12, out=out)
+    assert (out[12:] == -3).all()
+    check_tree(dict(c, q=c["q"][:12], offs=np.array([0, 12]), seen=c["seen"][:12, :12]), out[:12])
+
+
+def test_tree_attention_passes_over_missing_pages():
+    """Positions without a page (-1, or a tile that the pool does not have) are not seen."""
+    c = tree_case(6, (4, 2, 64), [64], [4], "bf16", kind="self")
+    full = run_tree(c)
+    short = dict(c, lens=[32])
+    c["table"][0][2:4] = [-1, 10 ** 6]
+    assert torch.equal(run_tree(c), run_tree(short)) and not torch.equal(full, run_tree(c))
+
+
+def test_tree_attention_layers():
+    c = tree_case(7, (4, 2, 64), [50, 3], [6, 4], "bf16")
+    pool = torch.cat([torch.randn_like(c["pool"].float()).to(torch.bfloat16), c["pool"], torch.randn_like(c["pool"].float()).to(torch.bfloat16)])
+    kv = sdlm.KvCache(pool.cuda(), page_table=dev(c["table"]), lengths=dev(c["lens"]))
+    out = sdlm.tree_attention(kv, 1, c["q"].cuda(), dev(c["offs"]), torch.from_numpy(c["mask"].copy()).cuda(), node_table=dev(c["ntab"]), max_nodes=6)
+    assert torch.equal(out, run_tree(c))
+
+
+def test_tree_attention_beyond_32_bit_offsets():
+    """A pool whose elements pass 2^31: the last tiles are read where they are (4.3 GB of zeros in front of them)."""
+    c = tree_case(8, (4, 2, 64), [70, 5], [9, 3], "bf16")
+    far = (1 << 31) // (2 * 2 * 16 * 64) + 5
+    pool = torch.zeros(1, far + c["pool"].shape[1], 2, 2, 16 * 64, dtype=torch.bfloat16, device="cuda")
+    pool[:, far:] = c["pool"].cuda()
+    kv = sdlm.KvCache(pool, page_table=dev(c["table"] + far), lengths=dev(c["lens"]))
+    out = sdlm.tree_attention(kv, 0, c["q"].cuda(), dev(c["offs"]), torch.from_numpy(c["mask"].copy()).cuda(), node_table=dev(c["ntab"] + far), max_nodes=9)
+    assert torch.equal(out, run_tree(c))
+
+
+# ---------------------------------------------------------------------------------------------------------------- forking
+
+def cache_case(seed, lens, ahead, pages, layers=2, heads=(2, 64), dtype="bf16", shared=None):
+    """Sequences whose pages come in random order; ahead: pages backed beyond what the length needs; shared: {sequence: (other, full pages it shares)}."""
+    rng = np.random.default_rng(seed)
+    hkv, d = heads
+    S = len(lens)
+    held = [-(-n // 16) + a for n, a in zip(lens, ahead)]
+    pps = max(held) + 2
+    free = list(rng.permutation(pages))
+    table = np.full((S, pps), -1)
+    refs = np.zeros(pages, int)
+    for b in range(S):
+        for j in range(held[b]):
+            other = (shared or {}).get(b)
+            page = table[other[0]][j] if other and j < other[1] else free.pop()
+            table[b, j] = page
+            refs[page] += 1
+    pool = torch.randn(layers, pages + 3, hkv, 2, 16 * d, generator=torch.Generator().manual_seed(seed)).to(DT[dtype])
+    return dict(table=table.astype(np.int32), lens=np.array(lens, np.int32), held=np.array(held, np.int32), refs=refs.astype(np.int32), pool=pool.float().numpy(), dtype=dtype)
+
+
+def kv_of(c):
+    pages = len(c["refs"])
+    pool = torch.from_numpy(c["pool"]).to(DT[c["dtype"]]).cuda()
+    t = dict(page_table=dev(c["table"]), lengths=dev(c["lens"]), backed=dev(c["held"]), page_refs=dev(c["refs"]), free_pages=torch.full((pages,), 99, dtype=torch.int32, device="cuda"),
+             free_count=torch.full((1,), 99, dtype=torch.int32, device="cuda"))
+    return sdlm.KvCache(pool, n_pages=pages, **t), pool, t
+
+
+def same_cache(want, pool, t):
+    for name, key in (("page_table", "table"), ("lengths", "lens"), ("backed", "held"), ("page_refs", "refs"), ("free_pages", "free")):
+        assert np.array_equal(t[name].cpu().numpy(), want[key]), name
+    assert t["free_count"].item() == want["n_free"]
+    assert np.array_equal(pool.float().cpu().numpy(), want["pool"])
+
+
+@pytest.mark.parametrize("share", [True, False])
+@pytest.mark.parametrize("parent", [[0, 0, 0, 0, 0], [0, 1, 2, 3, 4], [4, 3, 2, 1, 0], [1, 1, 2, 2, 2], [3, 3, 0, 0, 3], [-1, 0, -1, 1], [2], [], [1, 2, 3, 4, 0], [4, 4, 4, 3, -1], [-1, -1, -1, -1, -1]])
+def test_fork(parent, share):
+    c = cache_case(len(parent), [37, 16, 0, 5, 64], [0, 1, 0, 2, 0], 40)
+    kv, pool, t = kv_of(c)
+    kv.fork(dev(np.array(parent, np.int32)), share=share)
+    kv.check()
+    same_cache(plain.fork(c, parent, share), pool, t)
+
+
+@pytest.mark.parametrize("dtype,heads,layers", [("fp32", (1, 32), 1), ("fp32", (3, 96), 5), ("bf16", (4, 128), 3), ("bf16", (1, 32), 2)])
+def test_fork_types(dtype, heads, layers):
+    c = cache_case(3, [100, 15, 1], [1, 0, 0], 30, layers=layers, heads=heads, dtype=dtype)
+    for share in (True, False):
+        kv, pool, t = kv_of(c)
+        kv.fork(dev([1, 0, 0]), share=share)
+        kv.check()
+        same_cache(plain.fork(c, [1, 0, 0], share), pool, t)
+
+
+def test_fork_of_shared_pages_again_and_again():
+    """A search that forks at every step: what is shared stays shared until its last holder is gone."""
+    c = cache_case(4, [50, 0, 0, 0, 0, 0], [0] * 6, 24)
+    kv, pool, t = kv_of(c)
+    rng = np.random.default_rng(4)
+    for step in range(12):
+        parent = [0] * 6 if step == 0 else [int(v) for v in rng.integers(0, 6, 6)]
+        want = plain.fork(c, parent, True)
+        assert not isinstance(want, int)
+        kv.fork(dev(parent))
+        kv.check()
+        same_cache(want, pool, t)
+        c = {**want, "dtype": c["dtype"]}
+
+
+@pytest.mark.parametrize("S,pages", [(1, 1), (3, 5000), (300, 2048), (1030, 4097)])
+def test_fork_of_many_sequences(S, pages):
+    rng = np.random.default_rng(S)
+    lens = rng.integers(0, 16 if S > 1 else 17, S)
+    lens[0] = 16
+    c = cache_case(S, list(lens), [0] * S, pages, layers=1, heads=(1, 32))
+    parent = [int(v) for v in rng.integers(-1, S, S)]
+    for share in (True, False):
+        kv, pool, t = kv_of(c)
+        kv.fork(dev(np.array(parent, np.int32)), share=share)
+        kv.check()
+        same_cache(plain.fork(c, parent, share), pool, t)
+
+
+@pytest.mark.parametrize("parent,code,kw", [([0, 0, 0], sdlm.ECAPACITY, {}), ([0, 3, 0], sdlm.EINVAL, {}), ([-2, 1, 2], sdlm.EINVAL, {}), ([0, 1, 2], sdlm.EINVAL, dict(page=77)), ([0, 1, 2], sdlm.EINVAL, dict(page=-1))])
+def test_fork_refused_changes_nothing(parent, code, kw):
+    c = cache_case(6, [100, 30, 1], [0, 0, 0], 12)          # 7 + 2 + 1 pages held, 2 free
+    if "page" in kw:
+        c["table"][0, 1] = kw["page"]
+    kv, pool, t = kv_of(c)
+    kv.fork(dev(parent), share="page" in kw)
+    with pytest.raises(sdlm.SdlmError) as e:
+        kv.check()
+    assert e.value.code == code
+    for name, key in (("page_table", "table"), ("lengths", "lens"), ("backed", "held"), ("page_refs", "refs")):
+        assert np.array_equal(t[name].cpu().numpy(), c[key])
+    assert (t["free_pages"] == 99).all() and t["free_count"].item() == 99
+    assert np.array_equal(pool.float().cpu().numpy(), c["pool"])
+
+
+# ---------------------------------------------------------------------------------------------------------------- compacting
+
+@pytest.mark.parametrize("dtype,heads,layers", [("bf16", (2, 64), 3), ("fp32", (1, 32), 1), ("fp32", (2, 128), 2), ("bf16", (3, 96), 2), ("bf16", (4, 128), 1)])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_compact(dtype, heads, layers, inplace):
+    rng = np.random.default_rng(7)
+    lens, nodes, P = [37, 0, 15, 16, 90], [12, 40, 3, 30, 64], 33
+    room = [-(-(n + m) // 16) - -(-n // 16) for n, m in zip(lens, nodes)]
+    c = cache_case(7, lens, room, 60, layers=layers, heads=heads, dtype=dtype)
+    glen = np.array([4, 33, 0, 1, 20], np.int32)
+    path = np.full((5, P), 10 ** 6, np.int32)
+    for b in range(5):
+        path[b, :glen[b]] = np.sort(rng.permutation(nodes[b])[:glen[b]])
+    spare = rng.permutation(np.flatnonzero(c["refs"] == 0))[:20].reshape(5, 4)
+    ntab = c["table"] if inplace else spare
+    base = c["lens"] if inplace else np.array([0, 3, 1, 0, 0])
+    kv, pool, t = kv_of(c)
+    kv.compact(dev(path), dev(glen), node_table=dev(ntab), node_base=dev(base))
+    want = plain.compact(c["pool"], c["table"], lens, path, glen, ntab, base)
+    assert np.array_equal(pool.float().cpu().numpy(), want)
+    assert np.array_equal(t["lengths"].cpu().numpy(), c["lens"])
+
+
+def test_compact_passes_over_what_has_no_page():
+    c = cache_case(8, [30, 16], [0, 0], 12)
+    kv, pool, t = kv_of(c)
+    ntab = np.array([[9, -1], [500, 9]], np.int32)
+    # sequence 0: node 17 has no page, position 32 has none either; sequence 1: position 16 has none, node -3 and nodes behind the table do not exist
+    kv.compact(dev([[2, 17, 3], [-3, 16, 40]]), dev([3, 3]), node_table=dev(ntab))
+    want = plain.compact(c["pool"], c["table"], [30, 16], [[2]], [1], ntab, [0])
+    assert np.array_equal(pool.float().cpu().numpy(), want)
+
+
+# ---------------------------------------------------------------------------------------------------------------- together, streams, graphs
+
+def drafted(seed, B=3, T=6, d=64, hkv=2, hq=4, V=211):
+    """What a program around a decoder holds in a round of drafting: a cache, drafted trees with K/V behind it, queries, logits of every node."""
+    c = tree_case(seed, (hq, hkv, d), [20, 33, 7][:B], [T] * B, "bf16", inplace=True)
+    z, rng = draw_logits(seed, B * T, V, "fp32")
+    return c, z, dev(rng.random(B * T), torch.float32)
+
+
+def one_round(kv, c, z, u, q, offs, mask, path, path_len, parent):
+    """Attention of the drafts, a token for every node, the accepted branch into the cache, the beam's next sequences."""
+    out = sdlm.tree_attention(kv, 0, q, offs, mask, node_table=kv._keep[1], node_base=kv._keep[2], max_nodes=c["max_nodes"])
+    ids, prob = sdlm.sample(z, u, top_k=torch.full((z.shape[0],), 20, dtype=torch.int32, device=z.device))
+    kv.compact(path, path_len, node_table=kv._keep[1], node_base=kv._keep[2])
+    kv._keep[2].add_(path_len)
+    kv.fork(parent)
+    return out, ids, prob
+
+
+def round_inputs(seed):
+    c, z, u = drafted(seed)
+    pages = c["pool"].shape[1]
+    held = [-(-(n + 6) // 16) for n in c["lens"]]
+    used = np.concatenate([c["table"][b, :held[b]] for b in range(3)])
+    refs = np.zeros(pages, np.int32)
+    refs[used] = 1
+    table = np.where(np.arange(c["table"].shape[1])[None] < np.array(held)[:, None], c["table"], -1)
+    cache = dict(table=table.astype(np.int32), lens=np.array(c["lens"], np.int32), held=np.array(held, np.int32), refs=refs, pool=c["pool"].float().numpy(), dtype="bf16")
+    kv, pool, t = kv_of(cache)
+    path, plen, parent = np.array([[0, 2, 5], [1, 3, 0], [4, 0, 0]], np.int32), np.array([3, 2, 1], np.int32), [1, 1, 0]
+    args = (c, z, u, c["q"].cuda(), dev(c["offs"]), torch.from_numpy(c["mask"].copy()).cuda(), dev(path), dev(plen), dev(parent))
+    moved = dict(cache, pool=plain.compact(cache["pool"], cache["table"], cache["lens"], path, plen, cache["table"], cache["lens"]), lens=cache["lens"] + plen)
+    return kv, pool, t, args, plain.fork(moved, parent, True)
+
+
+def test_a_round_of_drafting_and_forking():
+    kv, pool, t, args, want = round_inputs(21)
+    out, ids, prob = one_round(kv, *args)
+    kv.check()
+    check_tree(args[0], out)
+    z, u = args[1], args[2]
+    assert ids.cpu().tolist() == [plain.sample_row(z[r].double().cpu().numpy(), 1.0, 20, 1.0, 0.0, float(u[r]))[0] for r in range(z.shape[0])]
+    same_cache(want, pool, t)
+
+
+def test_two_streams_at_once():
+    """Two rounds on streams of their own, each with its own cache: neither waits for the other, nor sees its scratch."""
+    alone = [one_round(r[0], *r[3]) for r in (round_inputs(31), round_inputs(32))]
+    torch.cuda.synchronize()
+    rounds, streams = [round_inputs(31), round_inputs(32)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for r, s in zip(rounds, streams):
+        with torch.cuda.stream(s):
+            got.append(one_round(r[0], *r[3]))
+    torch.cuda.synchronize()
+    for a, g, r in zip(alone, got, rounds):
+        assert all(torch.equal(x, y) for x, y in zip(a, g))
+        same_cache(r[4], r[1], r[2])
+
+
+def test_replays_of_captured_calls():
+    """Two graphs, captured one after the other and replayed in turn with eager calls between: each replay is the eager result on what the inputs hold then."""
+    z = [draw_logits(s, 5, 20011, "fp32")[0].clone() for s in (1, 2)]
+    u = [torch.rand(5, device="cuda") for _ in range(2)]
+    k = torch.full((5,), 40, dtype=torch.int32, device="cuda")
+    cs = [tree_case(s, (12, 2, 128), [700, 90], [9, 20], "bf16") for s in (41, 42)]
+    kvs = [sdlm.KvCache(c["pool"].cuda(), page_table=dev(c["table"]), lengths=dev(c["lens"])) for c in cs]
+    ins = [(c["q"].cuda(), dev(c["offs"]), torch.from_numpy(c["mask"].copy()).cuda(), dev(c["ntab"])) for c in cs]
+
+    def call(i):
+        ids, prob = sdlm.sample(z[i], u[i], top_k=k)
+        ids2, _ = sdlm.sample(z[i], u[i])
+        out = sdlm.tree_attention(kvs[i], 0, *ins[i][:3], node_table=ins[i][3], max_nodes=20)
+        return ids, prob, ids2, out
+
+    for i in range(2):
+        call(i)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call(i))
+        graphs.append(g)
+    rng = np.random.default_rng(0)
+    for n in range(4):
+        for i in range(2):
+            u[i].copy_(dev(rng.random(5), torch.float32))
+            z[i].add_(dev(rng.random((5, 20011)), torch.float32))
+            ins[i][0].mul_(-1)
+            kvs[i]._keep[2].copy_(dev([int(rng.integers(0, 700)), int(rng.integers(0, 90))]))
+        for i in (n % 2, 1 - n % 2):
+            graphs[i].replay()
+        want = [call(0), call(1)]
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i])), (n, i)
+
+
+def test_a_captured_fork():
+    """A fork in a graph, replayed on a cache that changes in between."""
+    kv, pool, t, args, _ = round_inputs(51)
+    parent = dev([0, 1, 2])
+    start = [x.clone() for x in (pool, *t.values())]
+    kv.fork(parent)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kv.fork(parent)
+    for p in ([1, 1, 0], [0, 0, 0], [2, 0, -1]):
+        for x, v in zip((pool, *t.values()), start):
+            x.copy_(v)
+        c = dict(table=t["page_table"].cpu().numpy(), lens=t["lengths"].cpu().numpy(), held=t["backed"].cpu().numpy(), refs=t["page_refs"].cpu().numpy(), pool=pool.float().cpu().numpy())
+        parent.copy_(dev(p))
+        g.replay()
+        kv.check()
+        same_cache(plain.fork(c, p, True), pool, t)
+
+
+def test_python_refusals():
+    z = torch.zeros(3, 50, device="cuda")
+    u = torch.zeros(3, device="cuda")
+    for bad in (dict(logits=z.half()), dict(logits=z.t()), dict(logits=z.cpu()), dict(u=u.double()), dict(u=u[:2]), dict(top_k=torch.zeros(3, device="cuda")), dict(temperature=torch.zeros(3))):
+        kw = dict(logits=z, u=u)
+        kw.update(bad)
+        with pytest.raises(sdlm.SdlmError) as e:
+            sdlm.sample(kw.pop("logits"), kw.pop("u"), **kw)
+        assert e.value.code == sdlm.EINVAL
+    c = tree_case(1, (4, 2, 64), [20], [4], "bf16")
+    for bad in (dict(q=c["q"].cuda().float()), dict(q=c["q"].cuda()[:, :3]), dict(q=c["q"]), dict(max_nodes=0), dict(max_nodes=2000), dict(out=torch.zeros(4, 4, 64, device="cuda"))):
+        with pytest.raises(sdlm.SdlmError) as e:
+            run_tree(c, **bad)
+        assert e.value.code == sdlm.EINVAL
+    with pytest.raises(sdlm.SdlmError):
+        sdlm.KvCache(c["pool"], page_table=dev(c["table"]), lengths=dev(c["lens"]))
+    kv = sdlm.KvCache(c["pool"].cuda(), page_table=dev(c["table"]), lengths=dev(c["lens"]))
+    with pytest.raises(sdlm.SdlmError):
+        kv.fork(dev([0]))
