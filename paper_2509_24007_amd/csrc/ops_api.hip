@@ -25,6 +25,8 @@ int launched(const char *what)
     return e == hipSuccess ? SDLM_OK : bad(SDLM_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+constexpr int MAX_TABLE = 1 << 26;   // entries of a sequence's table: positions fit 31 bits
+
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 int check_workspace(const void *w, size_t have, size_t need)
@@ -42,7 +44,7 @@ int check_kv(const sdlm_kv *kv, bool pages)
     if (kv->dtype != 0 && kv->dtype != 1) return bad(SDLM_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
     if (kv->head_dim != 32 && kv->head_dim != 64 && kv->head_dim != 96 && kv->head_dim != 128) return bad(SDLM_EINVAL, "head_dim must be 32, 64, 96 or 128");
     if (kv->n_layers < 1 || kv->n_tiles < 1 || kv->n_kv_heads < 1 || kv->max_seqs < 1 || kv->pages_per_seq < 1) return bad(SDLM_EINVAL, "bad cache sizes");
-    if (kv->pages_per_seq > (1 << 26)) return bad(SDLM_EINVAL, "pages_per_seq is at most %d", 1 << 26);
+    if (kv->pages_per_seq > MAX_TABLE) return bad(SDLM_EINVAL, "pages_per_seq is at most %d", MAX_TABLE);
     if ((long)kv->n_layers * kv->n_kv_heads > (1l << 30)) return bad(SDLM_EINVAL, "too many layers and heads");
     if (kv->layer_stride < (int64_t)(kv->n_layers > 1 ? kv->n_tiles : 0) * kv->n_kv_heads * 2 * PAGE * kv->head_dim || kv->layer_stride % (kv->dtype == 0 ? 4 : 8))
         return bad(SDLM_EINVAL, "layer_stride must hold the tiles of a layer and be a multiple of 16 bytes");
@@ -106,7 +108,7 @@ int sdlm_tree_attention(const sdlm_kv *kv, int32_t layer, const sdlm_tree_args *
     if (t->n_seqs > kv->max_seqs) return bad(SDLM_EINVAL, "%d sequences, the cache has %d", t->n_seqs, kv->max_seqs);
     if (t->n_rows < 0 || (long)t->n_rows > (long)t->n_seqs * t->max_nodes) return bad(SDLM_EINVAL, "%d rows for %d sequences of at most %d nodes", t->n_rows, t->n_seqs, t->max_nodes);
     if (t->mask_words < (t->max_nodes + 63) / 64) return bad(SDLM_EINVAL, "mask_words is too small for max_nodes");
-    if (t->node_pages < 1) return bad(SDLM_EINVAL, "node_pages must be at least 1");
+    if (t->node_pages < 1 || t->node_pages > MAX_TABLE) return bad(SDLM_EINVAL, "node_pages must be 1 .. %d", MAX_TABLE);
     const int64_t row = (int64_t)t->n_q_heads * kv->head_dim, vec = kv->dtype == 0 ? 4 : 8;
     if (t->q_stride < row || t->out_stride < row || t->q_stride % vec || t->out_stride % vec) return bad(SDLM_EINVAL, "q_stride and out_stride must hold a row and be multiples of 16 bytes");
     if (t->n_rows == 0 || t->n_seqs == 0) return SDLM_OK;
@@ -136,7 +138,8 @@ int sdlm_kv_compact(const sdlm_kv *kv, int32_t n_seqs, const int32_t *path, int3
     const int rc = check_kv(kv, false);
     if (rc) return rc;
     if (n_seqs < 0 || n_seqs > kv->max_seqs || n_seqs > 65535) return bad(SDLM_EINVAL, "%d sequences, the cache has %d (at most 65535 in a call)", n_seqs, kv->max_seqs);
-    if (max_path < 0 || path_stride < max_path || node_pages < 1) return bad(SDLM_EINVAL, "path_stride must hold max_path >= 0 nodes, and node_pages be at least 1");
+    if (max_path < 0 || path_stride < max_path || node_pages < 1 || node_pages > MAX_TABLE)
+        return bad(SDLM_EINVAL, "path_stride must hold max_path >= 0 nodes, and node_pages be 1 .. %d", MAX_TABLE);
     if (n_seqs == 0 || max_path == 0) return SDLM_OK;
     if (!path || !path_len || !node_table) return bad(SDLM_EINVAL, "path, path_len and node_table are required");
     launch_compact((hipStream_t)hip_stream, *kv, kv->lengths, node_table, node_pages, node_base, path, path_stride, path_len, n_seqs, max_path);

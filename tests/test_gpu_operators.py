@@ -190,6 +190,32 @@ def check_tree(c, out):
     assert worst <= 1.0, worst
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_tree_attention_non_finite_nodes(value, dtype):
+    """A node whose K or V are not finite: those that do not see it are what they would be without it, those that do are not finite (V: in the features where it is not)."""
+    c = tree_case(10, (6, 2, 64), [21, 0], [7, 40], dtype, kind="tree")
+    ref = run_tree(c)
+    i = np.arange(64)
+    for b, j in ((0, 2), (1, 17)):
+        clean = c["pool"].clone()
+        at = c["ntab"][b][j // 16]
+        sees = np.zeros(47, bool)
+        sees[c["offs"][b]:c["offs"][b + 1]] = c["seen"][c["offs"][b]:c["offs"][b + 1], j]
+        sees = torch.from_numpy(sees).cuda()
+        c["pool"][0, at, 1, 1, plain.v_index(j % 16, i[5:9])] = value         # features 5 to 8 of kv head 1: query heads 3 to 5
+        out = run_tree(c)
+        assert torch.equal(out[~sees], ref[~sees]) and sees.any()
+        assert not torch.isfinite(out[sees][:, 3:, 5:9]).any()
+        assert torch.equal(out[sees][:, :3], ref[sees][:, :3]) and torch.equal(out[sees][:, 3:, 9:], ref[sees][:, 3:, 9:])
+        c["pool"] = clean.clone()
+        if math.isnan(value):
+            c["pool"][0, at, 0, 0, plain.k_index(j % 16, i[:1])] = value
+            out = run_tree(c)
+            assert torch.equal(out[~sees], ref[~sees]) and torch.isnan(out[sees][:, :3]).all() and torch.equal(out[sees][:, 3:], ref[sees][:, 3:])
+        c["pool"] = clean
+
+
 HEADS = [(4, 2, 64), (12, 2, 128), (7, 1, 128), (8, 8, 32), (15, 3, 96)]
 
 
@@ -275,8 +301,11 @@ def test_tree_attention_passes_over_missing_pages():
     c = tree_case(6, (4, 2, 64), [64], [4], "bf16", kind="self")
     full = run_tree(c)
     short = dict(c, lens=[32])
+    check_tree(short, run_tree(short))
     c["table"][0][2:4] = [-1, 10 ** 6]
-    assert torch.equal(run_tree(c), run_tree(short)) and not torch.equal(full, run_tree(c))
+    out = run_tree(c)
+    check_tree(short, out)      # as without those positions, up to the order of the sums
+    assert not torch.equal(full, out)
 
 
 def test_tree_attention_layers():
