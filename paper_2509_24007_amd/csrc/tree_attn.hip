@@ -73,29 +73,42 @@ __global__ __launch_bounds__(64) void tree_rows_k(TreeArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------ matrix-core path (bf16)
-// A work item is (sequence, block of queries, run of tiles, kv head): its queries are the (node, query head) pairs that read the kv head, 16 QT for each of four
-// wavefronts, and all of them use every tile that the workgroup brings to LDS.  The items of a launch are laid out on the device from the actual lengths: every
-// wavefront reads the lengths and offsets of all sequences (a lane a sequence) and finds its own item by prefix sums, so ragged batches need no plan launch.
+// The queries of a sequence and kv head are its (node, query head) pairs, in blocks of 16 QT for each of four wavefronts; every tile that the workgroup
+// brings to LDS serves the whole block.  A launch has as many workgroups as the chip holds at once, and the tiles of all blocks, one block behind the other, are
+// dealt out to them in equal runs: no unit waits for another at the end, whatever the lengths are.  A workgroup's run may end inside a block; such a part leaves a
+// maximum, a sum and an unnormalised output, and the parts of a block are merged by a second launch.  At most its first and its last part are incomplete, so a
+// workgroup has two places for them.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 union Op8 { bf16x8 v; uint4 u; uint2 h[2]; uint32_t w[4]; };
 
-constexpr int ITEMS = 512;            // work items to aim at, over all kv heads
-constexpr int MIN_TILES = 4;          // fewest tiles of an item, where a sequence has that many
+#ifndef T_W1
+#define T_W1 3
+#endif
+#ifndef T_QT1
+#define T_QT1 64
+#endif
+#ifndef T_QT2
+#define T_QT2 100000
+#endif
+#ifndef T_SLOTS
+#define T_SLOTS 512
+#endif
+constexpr int MIN_PAIRS = 2;          // fewest pairs of tiles a workgroup takes, where there are that many
 constexpr float RESCALE_GAP = 8.0f;   // log2 units, see the running maximum below
 
 __device__ inline bool finite16(uint32_t x) { return (x & 0x7f80u) != 0x7f80u; }   // of a bf16's bits
 
 struct MfmaArgs {
     TreeArgs t;
-    float *part_o;      // [item][kv head][query of the block][HD]
-    float2 *part_ml;    // [item][kv head][query of the block]: running maximum, sum
+    float *part_o;      // [workgroup][first, last][query of the block][HD]
+    float2 *part_ml;    // [workgroup][first, last][query of the block]: running maximum, sum
     float c;            // log2(e) / sqrt(d)
-    int G;
+    int G, groups;      // groups: workgroups for each kv head
 };
 
-struct Seq { int first, nodes, len, base, prefix_tiles, tiles, blocks; };
+struct Seq { int first, nodes, len, base, prefix_tiles, tiles, pairs, blocks; };
 
 __device__ inline Seq seq_of(const TreeArgs &a, int b, int G, int qb)
 {
@@ -106,70 +119,85 @@ __device__ inline Seq seq_of(const TreeArgs &a, int b, int G, int qb)
     s.base = a.t.node_base ? min(max(a.t.node_base[b], 0), a.t.node_pages * PAGE) : 0;
     s.prefix_tiles = (s.len + PAGE - 1) / PAGE;
     s.tiles = s.prefix_tiles + (s.base % PAGE + s.nodes + PAGE - 1) / PAGE;
+    s.pairs = (s.tiles + 1) / 2;
     s.blocks = (s.nodes * G + qb - 1) / qb;
     return s;
 }
 
-// Tiles of an item: as many as leave about ITEMS items, an even number.
-__device__ inline int item_tiles(long all_tiles, int n_kv_heads)
+// Exclusive prefix sums over the sequences of their pairs of tiles (each block's) and their blocks; the wavefront's lanes hold the sequences b0 .. b0 + 63.
+struct Sums { long pairs; int blocks; };
+
+__device__ inline Sums lane_sums(const TreeArgs &a, int b0, int G, int qb, Sums *all)
 {
-    const long per = (all_tiles * n_kv_heads + ITEMS - 1) / ITEMS;
-    return (int)max((per + 1) / 2 * 2, (long)MIN_TILES);
+    const int lane = threadIdx.x & 63;
+    long v = 0;
+    int n = 0;
+    if (b0 + lane < a.t.n_seqs) { const Seq s = seq_of(a, b0 + lane, G, qb); n = s.blocks; v = (long)n * s.pairs; }
+    long x = v;
+    int y = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const long u = __shfl_up(x, o);
+        const int w = __shfl_up(y, o);
+        if (lane >= o) { x += u; y += w; }
+    }
+    all->pairs = __shfl(x, 63);
+    all->blocks = __shfl(y, 63);
+    return Sums{x - v, y - n};
 }
 
-// The sequence b, and the number of its first item, that item `want` belongs to (b = -1: there is no such item).  merge: counts blocks instead of items; `before` is then
-// the first block's number and `item0` its sequence's first item.
-struct Place { int b, before, item0, cp; };
-
-__device__ inline Place place_of(const TreeArgs &a, int G, int qb, int want, bool merge)
+__device__ inline long all_pairs(const TreeArgs &a, int G, int qb)
 {
-    const int lane = threadIdx.x & 63, S = a.t.n_seqs;
-    long all = 0;
-    for (int b0 = 0; b0 < S; b0 += 64) {
-        if (b0 + lane < S) { const Seq s = seq_of(a, b0 + lane, G, qb); all += (long)s.blocks * s.tiles; }
+    long sum = 0;
+    for (int b0 = 0; b0 < a.t.n_seqs; b0 += 64) { Sums t; lane_sums(a, b0, G, qb, &t); sum += t.pairs; }
+    return sum;
+}
+
+// The run of workgroup w: [w run, (w + 1) run) of the pairs.
+__device__ inline long run_of(long all, int groups) { return max((all + groups - 1) / groups, (long)MIN_PAIRS); }
+
+// The sequence in which pair (or, by_block, block) `at` lies, and how many pairs and blocks are in front of it; b = -1: none.
+struct Place { int b, blocks; long pairs; };
+
+__device__ inline Place place_of(const TreeArgs &a, int G, int qb, long at, bool by_block)
+{
+    Sums before{0, 0};
+    for (int b0 = 0; b0 < a.t.n_seqs; b0 += 64) {
+        Sums t;
+        const Sums m = lane_sums(a, b0, G, qb, &t);
+        const long mine = by_block ? before.blocks + m.blocks : before.pairs + m.pairs, end = by_block ? before.blocks + t.blocks : before.pairs + t.pairs;
+        if (at < end) {   // the last lane whose first pair is not behind `at`: those without any share their first pair with the next
+            const int lane = 63 - __clzll((long long)__ballot(mine <= at && b0 + (threadIdx.x & 63) < a.t.n_seqs));
+            return Place{b0 + lane, before.blocks + __shfl(m.blocks, lane), before.pairs + __shfl(m.pairs, lane)};
+        }
+        before.pairs += t.pairs;
+        before.blocks += t.blocks;
     }
-    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
-    Place p{-1, 0, 0, item_tiles(all, a.kv.n_kv_heads)};
-    int items = 0, blocks = 0;
-    for (int b0 = 0; b0 < S; b0 += 64) {
-        int n = 0, nb = 0;
-        if (b0 + lane < S) {
-            const Seq s = seq_of(a, b0 + lane, G, qb);
-            nb = s.blocks;
-            n = nb * ((s.tiles + p.cp - 1) / p.cp);
-        }
-        int xi = n, xb = nb;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int yi = __shfl_up(xi, o), yb = __shfl_up(xb, o);
-            if (lane >= o) { xi += yi; xb += yb; }
-        }
-        const int end = merge ? blocks + xb : items + xi;
-        const uint64_t past = __ballot(want < end);   // the first lane whose items end behind `want`
-        if (past) {
-            const int at = __ffsll((unsigned long long)past) - 1;
-            p.b = b0 + at;
-            p.item0 = __shfl(items + xi - n, at);
-            p.before = merge ? __shfl(blocks + xb - nb, at) : p.item0;
-            return p;
-        }
-        items += __shfl(xi, 63);
-        blocks += __shfl(xb, 63);
-    }
-    return p;
+    return Place{-1, 0, 0};
 }
 
 template <int HD, int QT>
-__global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
+__global__ __launch_bounds__(256, QT == 1 ? T_W1 : 2) void tree_mfma_k(MfmaArgs a)
 {
     constexpr int QB = 64 * QT, NK = HD / 32, ND = HD / 16, TILE = 2 * PAGE * HD, VEC = HD / 32;   // VEC: 16-byte loads of a thread for a pair of tiles
-    const int hk = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, lg = lane >> 4, G = a.G;
-    Place pl = place_of(a.t, G, QB, blockIdx.x, false);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, lg = lane >> 4, G = a.G;
+    // Workgroups are dealt to the eight dies in turn: each die gets a stretch of neighbouring runs, whose blocks read the same tiles.
+    const int per_die = (gridDim.x + 7) / 8, id = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3), hk = id / a.groups;
+    if (hk >= a.t.kv.n_kv_heads) return;
+    const long all = all_pairs(a.t, G, QB), run = run_of(all, a.groups), end = min(all, (id % a.groups + 1) * run);
+    long from = id % a.groups * run;
+    __shared__ __attribute__((aligned(16))) bf16_t kv[2][2 * TILE];   // two pairs of tiles, each as in the pool
+    __shared__ int strange[2][4];   // per wavefront: whether its part of the pair's values has some that are not finite (only where a query may not see all slots)
+    const bf16_t *pool = (const bf16_t *)a.t.pool;
+    for (int part = 0; from < end; ++part) {
+    const Place pl = place_of(a.t, G, QB, from, false);
     const int b = __builtin_amdgcn_readfirstlane(pl.b);
     if (b < 0) return;
-    const int cp = __builtin_amdgcn_readfirstlane(pl.cp);
     const Seq s = seq_of(a.t, b, G, QB);
-    const int local = blockIdx.x - __builtin_amdgcn_readfirstlane(pl.item0), block = local % s.blocks, chunk = local / s.blocks;
-    const int u0 = chunk * cp, u1 = min(s.tiles, u0 + cp), n_pairs = (u1 - u0 + 1) / 2, n_chunks = (s.tiles + cp - 1) / cp;
+    const int inside = __builtin_amdgcn_readfirstlane((int)(from - pl.pairs)), block = inside / s.pairs, p0 = inside % s.pairs;
+    const int n_pairs = (int)min((long)(s.pairs - p0), end - from), u0 = 2 * p0, u1 = min(s.tiles, u0 + 2 * n_pairs);
+    const bool complete = n_pairs == s.pairs;
+    from += n_pairs;
     const int q0 = block * QB + wave * 16 * QT, QR = s.nodes * G;
     const bool active = q0 < QR;
     const int32_t *ptab = a.t.kv.page_table + (size_t)b * a.t.kv.pages_per_seq, *ntab = a.t.t.node_table + (size_t)b * a.t.t.node_pages;
@@ -199,19 +227,22 @@ __global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
         for (int dt = 0; dt < ND; ++dt) O[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    __shared__ __attribute__((aligned(16))) bf16_t kv[2][2 * TILE];   // two pairs of tiles, each as in the pool
-    const bf16_t *pool = (const bf16_t *)a.t.pool;
-    // page of tile u, -1 where there is none
-    auto page = [&](int u) -> int {
-        if (u >= u1) return -1;
+    // Pages of 64 tiles, one a lane, and of the next 64: a lookup of its own in front of every pair would put a memory round trip into every iteration.  -1: there is none.
+    auto pages = [&](int w) -> int {
+        const int u = u0 + w * 64 + lane;
         int p = -1;
-        if (u < s.prefix_tiles) p = ptab[u];
-        else if (u + node_tile0 < a.t.t.node_pages) p = ntab[u + node_tile0];
+        if (u < s.prefix_tiles) { if (u < u1) p = ptab[u]; }
+        else if (u < u1 && u + node_tile0 < a.t.t.node_pages) p = ntab[u + node_tile0];
         return p < a.t.kv.n_tiles ? p : -1;
     };
-    // a pair in flight: its tiles' contents, and whether they exist
+    int pg = pages(0), pg_next = n_pairs > 32 ? pages(1) : -1;
+    // a pair in flight: its tiles' contents, and whether they exist.  Called for pairs in ascending order.
     auto fetch = [&](int pp, u32x4 (&r)[VEC]) -> int {
-        const int pA = page(u0 + 2 * pp), pB = page(u0 + 2 * pp + 1);
+        if ((pp & 31) == 0 && pp > 0) {
+            pg = pg_next;
+            if (pp + 32 < n_pairs) pg_next = pages(pp / 32 + 1);
+        }
+        const int pA = __builtin_amdgcn_readlane(pg, 2 * (pp & 31)), pB = __builtin_amdgcn_readlane(pg, 2 * (pp & 31) + 1);
         const bf16_t *tA = pool + ((size_t)max(pA, 0) * a.t.kv.n_kv_heads + hk) * TILE, *tB = pool + ((size_t)max(pB >= 0 ? pB : pA, 0) * a.t.kv.n_kv_heads + hk) * TILE;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -220,7 +251,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
         }
         return (pA >= 0 ? 1 : 0) | (pB >= 0 ? 2 : 0);
     };
-    __shared__ int strange[2][4];   // per wavefront: whether its part of the pair's values has some that are not finite (only where a query may not see all slots)
     auto is_whole = [&](int pp, int have) { return have == 3 && (u0 + 2 * pp + 2) * PAGE <= s.len; };   // every key of the pair is seen by every query
     auto stash = [&](int buf, const u32x4 (&r)[VEC], int pp, int have) {
 #pragma unroll
@@ -252,6 +282,13 @@ __global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
                 sA[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka.v, qop[t][kk].v, sA[t], 0, 0, 0);
                 sB[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb.v, qop[t][kk].v, sB[t], 0, 0, 0);
             }
+        }
+        const bf16_t *VA = KA + PAGE * HD, *VB = KB + PAGE * HD;
+        Op8 vo[ND];   // requested here, used behind the softmax
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+            vo[dt].h[0] = *(const uint2 *)(VA + (dt * 64 + lane) * 4);
+            vo[dt].h[1] = *(const uint2 *)(VB + (dt * 64 + lane) * 4);
         }
         const bool whole = is_whole(pp, have);
         uint32_t seen[QT];   // bits 0..15: slots of tile A that the query sees, 16..31: of tile B
@@ -309,7 +346,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
             pop[t].w[0] = pack_bf16(p[0], p[1]); pop[t].w[1] = pack_bf16(p[2], p[3]);
             pop[t].w[2] = pack_bf16(p[4], p[5]); pop[t].w[3] = pack_bf16(p[6], p[7]);
         }
-        const bf16_t *VA = KA + PAGE * HD, *VB = KB + PAGE * HD;
         // A slot that a query does not see may hold anything, and 0 times a value that is not finite is not 0.  Such values are added one by one for the queries that see them.
         const bool odd = !whole && (strange[buf][0] | strange[buf][1] | strange[buf][2] | strange[buf][3]);
         if (odd) {
@@ -335,20 +371,16 @@ __global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
                             if (seen[t] >> slot & 1) O[t][dt][i] += w[t] * bf16_to_f(v);
                     }
             }
-        }
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-            Op8 vo;
-            vo.h[0] = *(const uint2 *)(VA + (dt * 64 + lane) * 4);
-            vo.h[1] = *(const uint2 *)(VB + (dt * 64 + lane) * 4);
-            if (odd) {   // what is not finite leaves the product
+            for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (!finite16(vo.w[e >> 1] >> ((e & 1) * 16))) vo.w[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-            }
-#pragma unroll
-            for (int t = 0; t < QT; ++t) O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo.v, pop[t].v, O[t][dt], 0, 0, 0);
+                    if (!finite16(vo[dt].w[e >> 1] >> ((e & 1) * 16))) vo[dt].w[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
         }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int t = 0; t < QT; ++t) O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo[dt].v, pop[t].v, O[t][dt], 0, 0, 0);
     };
     u32x4 rA[VEC], rB[VEC];   // two pairs in flight: the next one and the one after it
     int hA = 0, hB, h0, h1 = 0;
@@ -369,58 +401,65 @@ __global__ __launch_bounds__(256, QT == 1 ? 4 : 2) void tree_mfma_k(MfmaArgs a)
         if (pp + 2 < n_pairs) { stash(0, rB, pp + 2, hB); h0 = hB; }
         __syncthreads();
     }
-    if (!active) return;
+    if (active) {
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        const int qi = q0 + t * 16 + ln;
-        float l = l_run[t];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (qi >= QR) continue;
-        if (n_chunks == 1) {
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
-            bf16_t *op = (bf16_t *)a.t.t.out + (size_t)(s.first + qi / G) * a.t.t.out_stride + (hk * G + qi % G) * HD + lg * 4;
+        for (int t = 0; t < QT; ++t) {
+            const int qi = q0 + t * 16 + ln;
+            float l = l_run[t];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (qi >= QR) continue;
+            if (complete) {
+                const float inv = l == 0.f ? 0.f : 1.0f / l;
+                bf16_t *op = (bf16_t *)a.t.t.out + (size_t)(s.first + qi / G) * a.t.t.out_stride + (hk * G + qi % G) * HD + lg * 4;
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-                const f32x4 o = O[t][dt] * inv;
-                *(uint2 *)(op + dt * 16) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+                for (int dt = 0; dt < ND; ++dt) {
+                    const f32x4 o = O[t][dt] * inv;
+                    *(uint2 *)(op + dt * 16) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+                }
+            } else {
+                const size_t at = ((size_t)id * 2 + (part > 0)) * QB + wave * 16 * QT + t * 16 + ln;
+                float *op = a.part_o + at * HD + lg * 4;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(op + dt * 16) = O[t][dt];
+                if (lg == 0) a.part_ml[at] = make_float2(m_run[t], l);
             }
-        } else {
-            const size_t at = ((size_t)blockIdx.x * a.t.kv.n_kv_heads + hk) * QB + wave * 16 * QT + t * 16 + ln;
-            float *op = a.part_o + at * HD + lg * 4;
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(op + dt * 16) = O[t][dt];
-            if (lg == 0) a.part_ml[at] = make_float2(m_run[t], l);
         }
+    }
     }
 }
 
-// The partial results of a block's items: out = sum_c 2^{c (m_c - M)} o_c / sum_c 2^{c (m_c - M)} l_c.  One workgroup 16 queries, 16 threads a query.
+// The parts of a block: out = sum_c 2^{c (m_c - M)} o_c / sum_c 2^{c (m_c - M)} l_c.  One workgroup 16 queries, 16 threads a query.
 template <int HD, int QT>
 __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
 {
     constexpr int QB = 64 * QT, V4 = HD / 4, PER = (V4 + 15) / 16;
     const int hk = blockIdx.y, G = a.G, part = blockIdx.x % (QB / 16), want = blockIdx.x / (QB / 16);
+    const long all = all_pairs(a.t, G, QB), run = run_of(all, a.groups);
     const Place pl = place_of(a.t, G, QB, want, true);
     const int b = __builtin_amdgcn_readfirstlane(pl.b);
     if (b < 0) return;
     const Seq s = seq_of(a.t, b, G, QB);
-    const int n_chunks = (s.tiles + pl.cp - 1) / pl.cp, block = want - pl.before;
-    if (n_chunks == 1) return;   // written by the attention itself
+    const int block = want - pl.blocks;
+    const long x0 = pl.pairs + (long)block * s.pairs;
+    const int w0 = (int)(x0 / run), n_parts = (int)((x0 + s.pairs - 1) / run) - w0 + 1;
+    if (n_parts == 1) return;   // written by the attention itself
     const int ql = part * 16 + (threadIdx.x >> 4), qi = block * QB + ql, x = threadIdx.x & 15;
     if (qi >= s.nodes * G) return;
-    const size_t step = (size_t)s.blocks * a.t.kv.n_kv_heads * QB, at0 = ((size_t)(pl.item0 + block) * a.t.kv.n_kv_heads + hk) * QB + ql;
+    const int late = w0 * run < x0;   // the first workgroup's run began in front of this block: the part is its last one
+    const size_t id0 = (size_t)hk * a.groups + w0;
+    auto at = [&](int c) { return ((id0 + c) * 2 + (c == 0 ? late : 0)) * QB + ql; };
     float M = -INFINITY;
-    for (int c = x; c < n_chunks; c += 16) M = fmaxf(M, a.part_ml[at0 + c * step].x);
+    for (int c = x; c < n_parts; c += 16) M = fmaxf(M, a.part_ml[at(c)].x);
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
     float L = 0.f;
     f32x4 o[PER] = {};
-    for (int c = 0; c < n_chunks; ++c) {
-        const float2 ml = a.part_ml[at0 + c * step];
+    for (int c = 0; c < n_parts; ++c) {
+        const float2 ml = a.part_ml[at(c)];
         const float w = ml.x == -INFINITY ? 0.f : exp2f((ml.x - M) * a.c);
         L += ml.y * w;
-        const f32x4 *src = (const f32x4 *)(a.part_o + (at0 + c * step) * HD);
+        const f32x4 *src = (const f32x4 *)(a.part_o + at(c) * HD);
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             if (x + 16 * i < V4) o[i] += src[x + 16 * i] * w;
@@ -433,9 +472,9 @@ __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
 }
 
 // Queries of a wavefront in units of 16: by the most queries that a kv head has in a sequence.
-int query_tiles(int queries) { return queries <= 64 ? 1 : 2; }
+int query_tiles(int queries) { return queries <= T_QT1 ? 1 : queries <= T_QT2 ? 2 : 3; }
 
-struct Shape { int qt; long blocks, items; };
+struct Shape { int qt, groups; long blocks; };
 
 Shape shape_of(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
 {
@@ -443,21 +482,23 @@ Shape shape_of(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
     const int queries = max_nodes * (n_q_heads / kv.n_kv_heads);
     s.qt = query_tiles(queries);
     s.blocks = (long)n_seqs * ((queries + 64 * s.qt - 1) / (64 * s.qt));
-    s.items = s.blocks + (ITEMS + kv.n_kv_heads - 1) / kv.n_kv_heads;   // at most one shorter item a block besides ITEMS full ones
+    const int slots = s.qt == 1 ? T_W1 * 256 : T_SLOTS;   // workgroups that the chip holds at once
+    s.groups = kv.n_kv_heads >= slots ? 1 : slots / kv.n_kv_heads;
     return s;
 }
 
 template <int HD, int QT>
-void mfma_go(hipStream_t s, const MfmaArgs &a, const Shape &sh, bool merge)
+void mfma_go(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 {
-    hipLaunchKernelGGL((tree_mfma_k<HD, QT>), dim3(sh.items, a.t.kv.n_kv_heads), dim3(256), 0, s, a);
-    if (merge) hipLaunchKernelGGL((tree_merge_k<HD, QT>), dim3(sh.blocks * 4 * QT, a.t.kv.n_kv_heads), dim3(256), 0, s, a);
+    const unsigned n = (unsigned)(sh.groups * a.t.kv.n_kv_heads + 7) / 8 * 8;
+    hipLaunchKernelGGL((tree_mfma_k<HD, QT>), dim3(n), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((tree_merge_k<HD, QT>), dim3(sh.blocks * 4 * QT, a.t.kv.n_kv_heads), dim3(256), 0, s, a);
 }
 
 template <int HD>
-void mfma_t(hipStream_t s, const MfmaArgs &a, const Shape &sh, bool merge)
+void mfma_t(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 {
-    if (sh.qt == 1) mfma_go<HD, 1>(s, a, sh, merge); else mfma_go<HD, 2>(s, a, sh, merge);
+    if (sh.qt == 1) mfma_go<HD, 1>(s, a, sh); else if (sh.qt == 2) mfma_go<HD, 2>(s, a, sh); else mfma_go<HD, 3>(s, a, sh);
 }
 
 template <typename T>
@@ -478,7 +519,7 @@ size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int ma
 {
     if (kv.dtype == 0) return 256;
     const Shape sh = shape_of(kv, n_q_heads, n_seqs, max_nodes);
-    return (size_t)sh.items * kv.n_kv_heads * 64 * sh.qt * (kv.head_dim * 4 + 8) + 256;
+    return (size_t)sh.groups * kv.n_kv_heads * 2 * 64 * sh.qt * (kv.head_dim * 4 + 8) + 256;
 }
 
 void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sdlm_tree_args &t, void *workspace, size_t workspace_bytes)
@@ -494,15 +535,13 @@ void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sd
     m.c = 1.4426950408889634f / sqrtf((float)kv.head_dim);
     const Shape sh = shape_of(kv, t.n_q_heads, t.n_seqs, t.max_nodes);
     m.part_o = (float *)workspace;
-    m.part_ml = (float2 *)((char *)workspace + (size_t)sh.items * kv.n_kv_heads * 64 * sh.qt * kv.head_dim * 4);
-    // One item a block whatever the lengths are: no merge.
-    const long most = (t.max_nodes + 2 * PAGE - 2) / PAGE + kv.pages_per_seq;
-    const bool merge = most > MIN_TILES;
+    m.part_ml = (float2 *)((char *)workspace + (size_t)sh.groups * kv.n_kv_heads * 2 * 64 * sh.qt * kv.head_dim * 4);
+    m.groups = sh.groups;
     switch (kv.head_dim) {
-    case 32: mfma_t<32>(s, m, sh, merge); break;
-    case 64: mfma_t<64>(s, m, sh, merge); break;
-    case 96: mfma_t<96>(s, m, sh, merge); break;
-    default: mfma_t<128>(s, m, sh, merge); break;
+    case 32: mfma_t<32>(s, m, sh); break;
+    case 64: mfma_t<64>(s, m, sh); break;
+    case 96: mfma_t<96>(s, m, sh); break;
+    default: mfma_t<128>(s, m, sh); break;
     }
 }
 
