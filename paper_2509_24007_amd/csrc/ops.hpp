@@ -11,6 +11,7 @@ void launch_sample(hipStream_t s, const sdlm_sample_args &a, void *workspace);
 
 // ---- attention of token trees over the cache (tree_attn.hip)
 constexpr int TREE_MAX_NODES = 1024;
+bool tree_fits(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes);   // the launch's counters hold them
 size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes, int max_len);
 void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sdlm_tree_args &t, void *workspace, size_t workspace_bytes);
 

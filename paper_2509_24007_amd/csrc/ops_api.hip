@@ -94,6 +94,10 @@ size_t sdlm_tree_attention_workspace_bytes(const sdlm_kv *kv, int32_t n_q_heads,
         bad(SDLM_EINVAL, "n_q_heads must be a multiple of n_kv_heads, max_nodes 1 .. %d, n_seqs and max_len not negative", TREE_MAX_NODES);
         return 0;
     }
+    if (!tree_fits(*kv, n_q_heads, n_seqs, max_nodes)) {
+        bad(SDLM_EINVAL, "%d sequences of %d pages with %d nodes each are too many for one launch", n_seqs, kv->pages_per_seq, max_nodes);
+        return 0;
+    }
     return tree_workspace_bytes(*kv, n_q_heads, n_seqs, max_nodes, max_len);
 }
 
@@ -111,6 +115,7 @@ int sdlm_tree_attention(const sdlm_kv *kv, int32_t layer, const sdlm_tree_args *
     if (t->node_pages < 1 || t->node_pages > MAX_TABLE) return bad(SDLM_EINVAL, "node_pages must be 1 .. %d", MAX_TABLE);
     const int64_t row = (int64_t)t->n_q_heads * kv->head_dim, vec = kv->dtype == 0 ? 4 : 8;
     if (t->q_stride < row || t->out_stride < row || t->q_stride % vec || t->out_stride % vec) return bad(SDLM_EINVAL, "q_stride and out_stride must hold a row and be multiples of 16 bytes");
+    if (!tree_fits(*kv, t->n_q_heads, t->n_seqs, t->max_nodes)) return bad(SDLM_EINVAL, "%d sequences of %d pages with %d nodes each are too many for one launch", t->n_seqs, kv->pages_per_seq, t->max_nodes);
     if (t->n_rows == 0 || t->n_seqs == 0) return SDLM_OK;
     if (!t->q || !t->out || !t->node_offsets || !t->mask || !t->node_table) return bad(SDLM_EINVAL, "q, out, node_offsets, mask and node_table are required");
     if (!aligned(t->q, 16) || !aligned(t->out, 16)) return bad(SDLM_EINVAL, "q and out must be 16-byte aligned");

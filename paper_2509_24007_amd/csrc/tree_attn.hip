@@ -83,18 +83,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 union Op8 { bf16x8 v; uint4 u; uint2 h[2]; uint32_t w[4]; };
 
-#ifndef T_W1
-#define T_W1 3
-#endif
-#ifndef T_QT1
-#define T_QT1 64
-#endif
-#ifndef T_QT2
-#define T_QT2 100000
-#endif
-#ifndef T_SLOTS
-#define T_SLOTS 512
-#endif
+constexpr int SLOTS = 512;            // workgroups that the chip holds at once, two a unit
 constexpr int MIN_PAIRS = 2;          // fewest pairs of tiles a workgroup takes, where there are that many
 constexpr float RESCALE_GAP = 8.0f;   // log2 units, see the running maximum below
 
@@ -103,7 +92,7 @@ __device__ inline bool finite16(uint32_t x) { return (x & 0x7f80u) != 0x7f80u; }
 struct MfmaArgs {
     TreeArgs t;
     float *part_o;      // [workgroup][first, last][query of the block][HD]
-    float2 *part_ml;    // [workgroup][first, last][query of the block]: running maximum, sum
+    float2 *part_ml;    // [workgroup][first, last][query of the block]: reference (log2), sum
     float c;            // log2(e) / sqrt(d)
     int G, groups;      // groups: workgroups for each kv head
 };
@@ -124,78 +113,84 @@ __device__ inline Seq seq_of(const TreeArgs &a, int b, int G, int qb)
     return s;
 }
 
-// Exclusive prefix sums over the sequences of their pairs of tiles (each block's) and their blocks; the wavefront's lanes hold the sequences b0 .. b0 + 63.
-struct Sums { long pairs; int blocks; };
+// The same in every lane, and known to be: loops and branches over it stay scalar.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-__device__ inline Sums lane_sums(const TreeArgs &a, int b0, int G, int qb, Sums *all)
+// Exclusive prefix sums over 64 sequences, a lane a sequence, of their pairs of tiles (each block's) and of their blocks, and the sums.  The pairs of a launch fit 31 bits (checked on the host).
+struct Sums { int pairs, blocks, all_pairs, all_blocks; };
+
+__device__ inline Sums lane_sums(const TreeArgs &a, int b0, int G, int qb)
 {
-    const int lane = threadIdx.x & 63;
-    long v = 0;
-    int n = 0;
-    if (b0 + lane < a.t.n_seqs) { const Seq s = seq_of(a, b0 + lane, G, qb); n = s.blocks; v = (long)n * s.pairs; }
-    long x = v;
-    int y = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const long u = __shfl_up(x, o);
-        const int w = __shfl_up(y, o);
-        if (lane >= o) { x += u; y += w; }
+    const int lane = threadIdx.x & 63, n = min(a.t.n_seqs - b0, 64);
+    int v = 0, w = 0;
+    if (lane < n) { const Seq s = seq_of(a, b0 + lane, G, qb); w = s.blocks; v = w * s.pairs; }
+    int x = v, y = w;
+    for (int o = 1; o < n; o <<= 1) {
+        const int u = __shfl_up(x, o), z = __shfl_up(y, o);
+        if (lane >= o) { x += u; y += z; }
     }
-    all->pairs = __shfl(x, 63);
-    all->blocks = __shfl(y, 63);
-    return Sums{x - v, y - n};
+    return Sums{x - v, y - w, __builtin_amdgcn_readlane(x, n - 1), __builtin_amdgcn_readlane(y, n - 1)};
 }
 
-__device__ inline long all_pairs(const TreeArgs &a, int G, int qb)
+// The run of workgroup w of a kv head: pairs w run .. (w + 1) run - 1.
+__device__ inline int run_of(int all, int groups) { return max((all + groups - 1) / groups, MIN_PAIRS); }
+
+__device__ inline int all_pairs(const TreeArgs &a, const Sums &first, int G, int qb)
 {
-    long sum = 0;
-    for (int b0 = 0; b0 < a.t.n_seqs; b0 += 64) { Sums t; lane_sums(a, b0, G, qb, &t); sum += t.pairs; }
+    int sum = first.all_pairs;
+    for (int b0 = 64; b0 < a.t.n_seqs; b0 += 64) sum += lane_sums(a, b0, G, qb).all_pairs;
     return sum;
 }
 
-// The run of workgroup w: [w run, (w + 1) run) of the pairs.
-__device__ inline long run_of(long all, int groups) { return max((all + groups - 1) / groups, (long)MIN_PAIRS); }
+// The sequence in which pair (or, by_block, block) `at` lies, and how many pairs and blocks are in front of it; b = -1: none.  first: the sums of the first 64 sequences.
+struct Place { int b, blocks, pairs; };
 
-// The sequence in which pair (or, by_block, block) `at` lies, and how many pairs and blocks are in front of it; b = -1: none.
-struct Place { int b, blocks; long pairs; };
-
-__device__ inline Place place_of(const TreeArgs &a, int G, int qb, long at, bool by_block)
+__device__ inline Place place_of(const TreeArgs &a, const Sums &first, int G, int qb, int at, bool by_block)
 {
-    Sums before{0, 0};
+    Sums m = first;
+    int pairs = 0, blocks = 0;
     for (int b0 = 0; b0 < a.t.n_seqs; b0 += 64) {
-        Sums t;
-        const Sums m = lane_sums(a, b0, G, qb, &t);
-        const long mine = by_block ? before.blocks + m.blocks : before.pairs + m.pairs, end = by_block ? before.blocks + t.blocks : before.pairs + t.pairs;
-        if (at < end) {   // the last lane whose first pair is not behind `at`: those without any share their first pair with the next
-            const int lane = 63 - __clzll((long long)__ballot(mine <= at && b0 + (threadIdx.x & 63) < a.t.n_seqs));
-            return Place{b0 + lane, before.blocks + __shfl(m.blocks, lane), before.pairs + __shfl(m.pairs, lane)};
+        if (b0) m = lane_sums(a, b0, G, qb);
+        if (at < (by_block ? blocks + m.all_blocks : pairs + m.all_pairs)) {   // the last lane whose first pair is not behind `at`: those without any share their first pair with the next
+            const uint64_t not_behind = __ballot((by_block ? blocks + m.blocks : pairs + m.pairs) <= at && b0 + (int)(threadIdx.x & 63) < a.t.n_seqs);
+            const int lane = 63 - __clzll((long long)not_behind);
+            return Place{b0 + lane, blocks + __builtin_amdgcn_readlane(m.blocks, lane), pairs + __builtin_amdgcn_readlane(m.pairs, lane)};
         }
-        before.pairs += t.pairs;
-        before.blocks += t.blocks;
+        pairs += m.all_pairs;
+        blocks += m.all_blocks;
     }
     return Place{-1, 0, 0};
 }
 
+__device__ inline float max3(float a, float b, float c)   // of results of vector instructions; a NaN loses
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 template <int HD, int QT>
-__global__ __launch_bounds__(256, QT == 1 ? T_W1 : 2) void tree_mfma_k(MfmaArgs a)
+__global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
 {
     constexpr int QB = 64 * QT, NK = HD / 32, ND = HD / 16, TILE = 2 * PAGE * HD, VEC = HD / 32;   // VEC: 16-byte loads of a thread for a pair of tiles
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, lg = lane >> 4, G = a.G;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), ln = lane & 15, lg = lane >> 4, G = a.G;
     // Workgroups are dealt to the eight dies in turn: each die gets a stretch of neighbouring runs, whose blocks read the same tiles.
     const int per_die = (gridDim.x + 7) / 8, id = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3), hk = id / a.groups;
     if (hk >= a.t.kv.n_kv_heads) return;
-    const long all = all_pairs(a.t, G, QB), run = run_of(all, a.groups), end = min(all, (id % a.groups + 1) * run);
-    long from = id % a.groups * run;
+    const Sums sums = lane_sums(a.t, 0, G, QB);
+    const int all = all_pairs(a.t, sums, G, QB), run = run_of(all, a.groups);
+    const int end = (int)min((long)all, (long)(id % a.groups + 1) * run);
+    int from = (int)min((long)all, (long)(id % a.groups) * run);
     __shared__ __attribute__((aligned(16))) bf16_t kv[2][2 * TILE];   // two pairs of tiles, each as in the pool
     __shared__ int strange[2][4];   // per wavefront: whether its part of the pair's values has some that are not finite (only where a query may not see all slots)
     const bf16_t *pool = (const bf16_t *)a.t.pool;
     for (int part = 0; from < end; ++part) {
-    const Place pl = place_of(a.t, G, QB, from, false);
-    const int b = __builtin_amdgcn_readfirstlane(pl.b);
+    const Place pl = place_of(a.t, sums, G, QB, from, false);
+    const int b = uniform(pl.b);
     if (b < 0) return;
     const Seq s = seq_of(a.t, b, G, QB);
-    const int inside = __builtin_amdgcn_readfirstlane((int)(from - pl.pairs)), block = inside / s.pairs, p0 = inside % s.pairs;
-    const int n_pairs = (int)min((long)(s.pairs - p0), end - from), u0 = 2 * p0, u1 = min(s.tiles, u0 + 2 * n_pairs);
+    const int inside = from - uniform(pl.pairs), block = inside / s.pairs, p0 = inside % s.pairs;
+    const int n_pairs = min(s.pairs - p0, end - from), u0 = 2 * p0, u1 = min(s.tiles, u0 + 2 * n_pairs);
     const bool complete = n_pairs == s.pairs;
     from += n_pairs;
     const int q0 = block * QB + wave * 16 * QT, QR = s.nodes * G;
@@ -246,8 +241,8 @@ __global__ __launch_bounds__(256, QT == 1 ? T_W1 : 2) void tree_mfma_k(MfmaArgs 
         const bf16_t *tA = pool + ((size_t)max(pA, 0) * a.t.kv.n_kv_heads + hk) * TILE, *tB = pool + ((size_t)max(pB >= 0 ? pB : pA, 0) * a.t.kv.n_kv_heads + hk) * TILE;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int e = tid + 256 * i;
-            r[i] = *(const u32x4 *)((e < TILE / 8 ? tA : tB - TILE) + (size_t)e * 8);
+            const bf16_t *t = wave * 64 + 256 * i < TILE / 8 ? tA : tB - TILE;   // a wavefront's part lies in one tile
+            r[i] = *(const u32x4 *)(t + (unsigned)(tid + 256 * i) * 8);
         }
         return (pA >= 0 ? 1 : 0) | (pB >= 0 ? 2 : 0);
     };
@@ -284,9 +279,9 @@ __global__ __launch_bounds__(256, QT == 1 ? T_W1 : 2) void tree_mfma_k(MfmaArgs 
             }
         }
         const bf16_t *VA = KA + PAGE * HD, *VB = KB + PAGE * HD;
-        Op8 vo[ND];   // requested here, used behind the softmax
+        Op8 vo[ND];
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
+        for (int dt = 0; dt < ND; ++dt) {   // requested here, used behind the softmax
             vo[dt].h[0] = *(const uint2 *)(VA + (dt * 64 + lane) * 4);
             vo[dt].h[1] = *(const uint2 *)(VB + (dt * 64 + lane) * 4);
         }
@@ -319,29 +314,40 @@ __global__ __launch_bounds__(256, QT == 1 ? T_W1 : 2) void tree_mfma_k(MfmaArgs 
                 }
             }
         }
-        Op8 pop[QT];
+        // Exponents of 2, against a reference that is a maximum of earlier scores: x = c s - ref.  It only moves when it is exceeded by more than RESCALE_GAP (2^x stays
+        // below 2^RESCALE_GAP, harmless in fp32 sums and bf16 products); only then is the maximum taken over the query's four lanes and are the accumulators rescaled.
+        float x[QT][8], mx[QT];
+        bool grows = false;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            // raw scores; the softmax scale is folded into the exponent: p = 2^(c s - c m).  The reference maximum only moves when it is exceeded by more than
-            // RESCALE_GAP / c (p stays below 2^RESCALE_GAP, harmless in fp32 sums and bf16 products); the accumulators are rescaled only then.
-            float mx = fmaxf(fmaxf(fmaxf(sA[t][0], sA[t][1]), fmaxf(sA[t][2], sA[t][3])), fmaxf(fmaxf(sB[t][0], sB[t][1]), fmaxf(sB[t][2], sB[t][3])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            if (__any((mx - m_run[t]) * a.c > RESCALE_GAP || (m_run[t] == -INFINITY && mx > -INFINITY))) {
-                const float m_new = fmaxf(m_run[t], mx);
-                const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[t] - m_new) * a.c);
+            const float ref = m_run[t] == -INFINITY ? 0.f : m_run[t];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) { x[t][v] = fmaf(sA[t][v], a.c, -ref); x[t][4 + v] = fmaf(sB[t][v], a.c, -ref); }
+            mx[t] = max3(max3(x[t][0], x[t][1], x[t][2]), max3(x[t][3], x[t][4], x[t][5]), max3(x[t][6], x[t][7], x[t][7]));
+            grows |= mx[t] > (m_run[t] == -INFINITY ? -INFINITY : RESCALE_GAP);
+        }
+        if (__any(grows)) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                const float ref = m_run[t] == -INFINITY ? 0.f : m_run[t];
+                mx[t] = fmaxf(mx[t], __shfl_xor(mx[t], 16));
+                mx[t] = fmaxf(mx[t], __shfl_xor(mx[t], 32));
+                const float m_new = fmaxf(m_run[t], mx[t] + ref);
+                const float to = m_new == -INFINITY ? 0.f : m_new, corr = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[t] - to);   // without a reference nothing has been added
                 l_run[t] *= corr;
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) O[t][dt] *= corr;
                 m_run[t] = m_new;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) { x[t][v] = fmaf(sA[t][v], a.c, -to); x[t][4 + v] = fmaf(sB[t][v], a.c, -to); }
             }
-            const float mc = m_run[t] == -INFINITY ? 0.f : m_run[t] * a.c;
+        }
+        Op8 pop[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
             float p[8];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                p[v] = __builtin_amdgcn_exp2f(fmaf(sA[t][v], a.c, -mc));
-                p[4 + v] = __builtin_amdgcn_exp2f(fmaf(sB[t][v], a.c, -mc));
-            }
+            for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(x[t][v]);
             l_run[t] += (p[0] + p[1]) + (p[2] + p[3]) + (p[4] + p[5]) + (p[6] + p[7]);
             pop[t].w[0] = pack_bf16(p[0], p[1]); pop[t].w[1] = pack_bf16(p[2], p[3]);
             pop[t].w[2] = pack_bf16(p[4], p[5]); pop[t].w[3] = pack_bf16(p[6], p[7]);
@@ -429,20 +435,20 @@ __global__ __launch_bounds__(256, QT == 1 ? T_W1 : 2) void tree_mfma_k(MfmaArgs 
     }
 }
 
-// The parts of a block: out = sum_c 2^{c (m_c - M)} o_c / sum_c 2^{c (m_c - M)} l_c.  One workgroup 16 queries, 16 threads a query.
+// The parts of a block: out = sum_c 2^{m_c - M} o_c / sum_c 2^{m_c - M} l_c.  One workgroup 16 queries, 16 threads a query.
 template <int HD, int QT>
 __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
 {
     constexpr int QB = 64 * QT, V4 = HD / 4, PER = (V4 + 15) / 16;
     const int hk = blockIdx.y, G = a.G, part = blockIdx.x % (QB / 16), want = blockIdx.x / (QB / 16);
-    const long all = all_pairs(a.t, G, QB), run = run_of(all, a.groups);
-    const Place pl = place_of(a.t, G, QB, want, true);
-    const int b = __builtin_amdgcn_readfirstlane(pl.b);
+    const Sums sums = lane_sums(a.t, 0, G, QB);
+    const int run = run_of(all_pairs(a.t, sums, G, QB), a.groups);
+    const Place pl = place_of(a.t, sums, G, QB, want, true);
+    const int b = uniform(pl.b);
     if (b < 0) return;
     const Seq s = seq_of(a.t, b, G, QB);
     const int block = want - pl.blocks;
-    const long x0 = pl.pairs + (long)block * s.pairs;
-    const int w0 = (int)(x0 / run), n_parts = (int)((x0 + s.pairs - 1) / run) - w0 + 1;
+    const int x0 = pl.pairs + block * s.pairs, w0 = x0 / run, n_parts = (x0 + s.pairs - 1) / run - w0 + 1;
     if (n_parts == 1) return;   // written by the attention itself
     const int ql = part * 16 + (threadIdx.x >> 4), qi = block * QB + ql, x = threadIdx.x & 15;
     if (qi >= s.nodes * G) return;
@@ -457,7 +463,7 @@ __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
     f32x4 o[PER] = {};
     for (int c = 0; c < n_parts; ++c) {
         const float2 ml = a.part_ml[at(c)];
-        const float w = ml.x == -INFINITY ? 0.f : exp2f((ml.x - M) * a.c);
+        const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
         L += ml.y * w;
         const f32x4 *src = (const f32x4 *)(a.part_o + at(c) * HD);
 #pragma unroll
@@ -471,8 +477,10 @@ __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
         if (x + 16 * i < V4) *(uint2 *)(op + (x + 16 * i) * 4) = make_uint2(pack_bf16(o[i][0] * inv, o[i][1] * inv), pack_bf16(o[i][2] * inv, o[i][3] * inv));
 }
 
-// Queries of a wavefront in units of 16: by the most queries that a kv head has in a sequence.
-int query_tiles(int queries) { return queries <= T_QT1 ? 1 : queries <= T_QT2 ? 2 : 3; }
+// Queries of a wavefront in units of 16: by the most queries that a kv head has in a sequence.  One for up to 64, so that all four wavefronts have some; beyond, two, which reads
+// every tile half as often from memory and LDS.  us, one / two: 64 sequences of 3072 positions, 7 queries 84 / 87, 56 queries 100 / 104, up to 112 queries 132 / 110;  4 trees of 1200 to
+// 2048 queries over 6144 positions 116 / 98.  Three would need more registers than two workgroups a unit leave (98 -> 122).
+int query_tiles(int queries) { return queries <= 64 ? 1 : 2; }
 
 struct Shape { int qt, groups; long blocks; };
 
@@ -482,8 +490,7 @@ Shape shape_of(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
     const int queries = max_nodes * (n_q_heads / kv.n_kv_heads);
     s.qt = query_tiles(queries);
     s.blocks = (long)n_seqs * ((queries + 64 * s.qt - 1) / (64 * s.qt));
-    const int slots = s.qt == 1 ? T_W1 * 256 : T_SLOTS;   // workgroups that the chip holds at once
-    s.groups = kv.n_kv_heads >= slots ? 1 : slots / kv.n_kv_heads;
+    s.groups = kv.n_kv_heads >= SLOTS ? 1 : SLOTS / kv.n_kv_heads;
     return s;
 }
 
@@ -498,7 +505,7 @@ void mfma_go(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 template <int HD>
 void mfma_t(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 {
-    if (sh.qt == 1) mfma_go<HD, 1>(s, a, sh); else if (sh.qt == 2) mfma_go<HD, 2>(s, a, sh); else mfma_go<HD, 3>(s, a, sh);
+    if (sh.qt == 1) mfma_go<HD, 1>(s, a, sh); else mfma_go<HD, 2>(s, a, sh);
 }
 
 template <typename T>
@@ -514,6 +521,12 @@ void rows_t(hipStream_t s, const TreeArgs &a)
 }
 
 }  // namespace
+
+bool tree_fits(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
+{
+    const long pairs = (kv.pages_per_seq + (max_nodes + 2 * PAGE - 2) / PAGE + 1) / 2, blocks = ((long)max_nodes * (n_q_heads / kv.n_kv_heads) + 63) / 64;
+    return (double)n_seqs * blocks * pairs < 2147000000.0;
+}
 
 size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes, int max_len)
 {

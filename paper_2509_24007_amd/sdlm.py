@@ -385,16 +385,16 @@ PAGE = 16
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _need(ok: bool, msg: str) -> None:
-    if not ok:
-        raise SdlmError(EINVAL, msg)
+def _refuse(msg: str) -> None:
+    raise SdlmError(EINVAL, msg)
 
 
 def _ints(t: Optional[torch.Tensor], n: int, name: str, dev, dtype=torch.int32) -> Optional[int]:
     """Address of a contiguous vector of at least n entries on the operator's device."""
     if t is None:
         return None
-    _need(t.dtype == dtype and t.device == dev and t.is_contiguous() and t.numel() >= n, f"{name} must be {n} or more contiguous {dtype} on {dev}")
+    if t.dtype is not dtype or t.device != dev or not t.is_contiguous() or t.numel() < n:
+        _refuse(f"{name} must be {n} or more contiguous {dtype} on {dev}")
     return t.data_ptr()
 
 
@@ -420,7 +420,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: Optional[torch
     """Draw one token from each row of logits [rows, vocab] (fp32 or bf16, the last dimension contiguous) with the uniform numbers u [rows]; the settings are
     vectors over the rows or None (see sdlm_sample in the header).  Returns ids [rows] int32 and their probabilities [rows] fp32.  Runs on the current stream."""
     L = load()
-    _need(logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be [rows, vocab] fp32 or bf16 on a GPU, the last dimension contiguous")
+    if not (logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1)):
+        _refuse("logits must be [rows, vocab] fp32 or bf16 on a GPU, the last dimension contiguous")
     R, V = logits.shape
     dev, f32 = logits.device, torch.float32
     stride = logits.stride(0) if R > 1 else V
@@ -430,7 +431,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: Optional[torch
                    _ints(top_p, R, "top_p", dev, f32), _ints(min_p, R, "min_p", dev, f32), _ints(u, R, "u", dev, f32), ids.data_ptr(), prob.data_ptr())
     if R:
         need = L.sdlm_sample_workspace_bytes(R, V)
-        _need(need > 0, f"{R} rows of {V} logits are outside the limits")
+        if not (need > 0):
+            _refuse(f"{R} rows of {V} logits are outside the limits")
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
         _run_op(dev, L.sdlm_sample, C.byref(a), ws.data_ptr(), need)
     return ids, prob
@@ -443,9 +445,12 @@ class KvCache:
 
     def __init__(self, pool: torch.Tensor, *, page_table: torch.Tensor, lengths: torch.Tensor, n_pages: int = 0, backed: Optional[torch.Tensor] = None,
                  page_refs: Optional[torch.Tensor] = None, free_pages: Optional[torch.Tensor] = None, free_count: Optional[torch.Tensor] = None):
-        _need(pool.is_cuda and pool.dim() == 5 and pool.dtype in _DTYPES and pool.shape[3] == 2 and pool.shape[4] % PAGE == 0, "pool must be [layers, tiles, kv heads, 2, 16 * head_dim] fp32 or bf16 on a GPU")
-        _need(pool[0].is_contiguous(), "a layer of the pool must be contiguous")
-        _need(page_table.dim() == 2, "page_table must be [sequences, pages a sequence]")
+        if not (pool.is_cuda and pool.dim() == 5 and pool.dtype in _DTYPES and pool.shape[3] == 2 and pool.shape[4] % PAGE == 0):
+            _refuse("pool must be [layers, tiles, kv heads, 2, 16 * head_dim] fp32 or bf16 on a GPU")
+        if not (pool[0].is_contiguous()):
+            _refuse("a layer of the pool must be contiguous")
+        if not (page_table.dim() == 2):
+            _refuse("page_table must be [sequences, pages a sequence]")
         self.device = dev = pool.device
         self.dtype, self.head_dim, self.n_kv_heads = pool.dtype, pool.shape[4] // PAGE, pool.shape[2]
         S, pps = page_table.shape
@@ -475,7 +480,8 @@ class KvCache:
     def compact(self, path: torch.Tensor, path_len: torch.Tensor, *, node_table: torch.Tensor, node_base: Optional[torch.Tensor] = None) -> None:
         """Move the K/V of nodes path[b, :path_len[b]] to the positions from lengths[b] on, in every layer; see sdlm_kv_compact."""
         dev = self.device
-        _need(path.dim() == 2 and node_table.dim() == 2 and node_table.shape[0] >= path.shape[0], "path must be [sequences, most nodes], node_table [sequences, pages]")
+        if not (path.dim() == 2 and node_table.dim() == 2 and node_table.shape[0] >= path.shape[0]):
+            _refuse("path must be [sequences, most nodes], node_table [sequences, pages]")
         S, P = path.shape
         _run_op(dev, load().sdlm_kv_compact, C.byref(self.desc), S, _ints(path, S * P, "path", dev), P, _ints(path_len, S, "path_len", dev), P,
                 _ints(node_table, 1, "node_table", dev), node_table.shape[1], _ints(node_base, S, "node_base", dev))
@@ -486,16 +492,21 @@ def tree_attention(kv: KvCache, layer: int, q: torch.Tensor, node_offsets: torch
     """Attention of drafted token trees over one layer of the cache (see sdlm_tree_attention): q [nodes, query heads, head_dim] of the cache's type, rows node_offsets[b] up to
     node_offsets[b + 1] belong to sequence b; mask [nodes, words] int64, bit j of a row: the node sees node j of its sequence.  Returns out, shaped as q."""
     L, dev = load(), kv.device
-    _need(q.dim() == 3 and q.shape[2] == kv.head_dim and q.dtype == kv.dtype and q.device == dev, "q must be [nodes, query heads, head_dim] of the cache's type and device")
-    _need(mask.dim() == 2 and node_table.dim() == 2, "mask must be [nodes, words], node_table [sequences, pages]")
+    if not (q.dim() == 3 and q.shape[2] == kv.head_dim and q.dtype == kv.dtype and q.device == dev):
+        _refuse("q must be [nodes, query heads, head_dim] of the cache's type and device")
+    if not (mask.dim() == 2 and node_table.dim() == 2):
+        _refuse("mask must be [nodes, words], node_table [sequences, pages]")
     N, H, d = q.shape
     S = node_offsets.numel() - 1
     if out is None:
         out = torch.empty(N, H, d, dtype=q.dtype, device=dev)
-    _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev, "out must be shaped as q, of its type and device")
+    if not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev):
+        _refuse("out must be shaped as q, of its type and device")
     for t in (q, out):
-        _need(t.stride(2) == 1 and (t.stride(1) == d or H == 1), "the heads of a row of q and out must be contiguous")
-    _need(S >= 0 and node_table.shape[0] >= S and mask.shape[0] >= N, "node_offsets, node_table and mask must agree with the nodes")
+        if not (t.stride(2) == 1 and (t.stride(1) == d or H == 1)):
+            _refuse("the heads of a row of q and out must be contiguous")
+    if not (S >= 0 and node_table.shape[0] >= S and mask.shape[0] >= N):
+        _refuse("node_offsets, node_table and mask must agree with the nodes")
     row = H * d
     a = TreeArgs(q.data_ptr(), out.data_ptr(), q.stride(0) if N > 1 else row, out.stride(0) if N > 1 else row, N, S, H, max_nodes, max_len,
                  _ints(node_offsets, S + 1, "node_offsets", dev), _ints(mask, N, "mask", dev, torch.int64), mask.shape[1], node_table.shape[1],
