@@ -1,10 +1,16 @@
 // Drawing tokens from logits: temperature, top-k, top-p, min-p and a given uniform number, row by row.
 //
-// The tokens of a row are ordered by logit, equal ones by index.  All filters keep a first part of that order, and the uniform number
-// picks from the kept part in that order, so the kernel never sorts: each step looks for the first token whose running count or
-// running weight passes a bound, by digits of the order-preserving integer of the logit.
-// Weights w = e^((z - max) / t) are integers in units of 2^-44 of the largest: their sums do not depend on the order of the threads,
-// and their error (2^-45 a token) is far below the weight of any token that a draw could fall on.
+// The tokens of a row are ordered by logit, equal ones by index.  All filters keep a first part of that order, and the uniform number picks from the kept part
+// in that order.  Weights are integers in units of 2^-44 of the largest (or of the power of two above it): their sums do not depend on the order of the threads, and
+// their error (2^-45 a token) is far below the weight of any token that a draw could fall on.
+//
+// Two launches.  The first reads the logits once, all units together: a thread takes 64 of them and leaves the maxima of its runs, and for a row whose filters need the
+// weight of the whole row (no top-k) a workgroup also leaves a histogram of the weights over 1/32 octaves.  The second has a workgroup a row, which sorts only what matters:
+//   - top-k: the k-th largest of the runs' maxima is no more than the k-th largest logit, so the candidates are what reaches it, in the few runs that do;
+//   - min-p: the candidates are what reaches min_p of the largest;
+//   - otherwise the histogram says in which bin the weight passes top_p, and in which bin the draw falls, and the candidates are that bin.
+// Where the candidates do not fit (thousands of equal logits), where top-k is beyond TOP_MAX, or where the exponents leave the histogram's range, the row is searched by digits
+// of the logits' order-preserving integers instead, without sorting, in a dozen passes.
 #include "ops.hpp"
 
 namespace sdlm {
@@ -14,6 +20,8 @@ namespace {
 constexpr int TH = 1024;
 typedef unsigned long long u64;
 constexpr double ONE = 17592186044416.0;   // 2^44
+constexpr double LOG2E = 1.4426950408889634;
+constexpr uint32_t KEY_NEG_INF = 0x007fffffu;
 
 __device__ inline float canon(float z)   // NaN is never drawn; the two zeros are equal
 {
@@ -85,28 +93,52 @@ __device__ Found search(Shared &sh, const Row<T> &row, const Weigh &w, int by, u
             const uint32_t k = key_of(z);
             if (z == -INFINITY || (shift < 24 && (k >> (shift + 8)) != prefix)) continue;
             atomicAdd(&sh.cnt[(k >> shift) & 255], 1u);
-            atomicAdd(&sh.mass[(k >> shift) & 255], w(z));
+            if (by != BY_COUNT) atomicAdd(&sh.mass[(k >> shift) & 255], w(z));
         }
         __syncthreads();
-        if (tid == 0) {
-            u64 m = sh.acc_mass, n = sh.acc_cnt;
-            int last = -1, d = 255;
-            for (; d >= 0; --d) {
-                if (!sh.cnt[d]) continue;
-                last = d;
-                const u64 m1 = m + sh.mass[d], n1 = n + sh.cnt[d];
-                if (by == BY_COUNT ? n1 >= bound : by == MASS_AT_LEAST ? m1 >= bound : m1 > bound) break;
-                m = m1; n = n1;
+        if (tid < 64) {   // lane l: digits 255 - 4 l .. 252 - 4 l
+            u64 m4[4], n4[4], m = 0, n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { m4[i] = sh.mass[255 - 4 * tid - i]; n4[i] = sh.cnt[255 - 4 * tid - i]; m += m4[i]; n += n4[i]; }
+            u64 ms = m, ns = n;
+            for (int o = 1; o < 64; o <<= 1) {
+                const u64 x = __shfl_up(ms, o), y = __shfl_up(ns, o);
+                if (tid >= o) { ms += x; ns += y; }
             }
-            if (d < 0) { d = last < 0 ? 0 : last; m -= sh.mass[d]; n -= sh.cnt[d]; }   // not passed: the last token
-            sh.prefix = prefix << 8 | d;
-            sh.acc_mass = m; sh.acc_cnt = n;
+            ms += sh.acc_mass; ns += sh.acc_cnt;
+            auto past = [&](u64 mass, u64 count) { return by == BY_COUNT ? count >= bound : by == MASS_AT_LEAST ? mass >= bound : mass > bound; };
+            u64 lanes = __ballot(n && past(ms, ns));
+            if (!lanes) lanes = 1ull << (63 - __clzll((long long)__ballot(n != 0)));   // not passed: the last token
+            if (tid == __ffsll(lanes) - 1) {
+                u64 mb = ms - m, nb = ns - n;
+                int last = 0;
+                u64 ml = mb, nl = nb;
+                bool found = false;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    if (found || !n4[d]) continue;
+                    last = d; ml = mb; nl = nb;
+                    found = past(mb + m4[d], nb + n4[d]);
+                    mb += m4[d]; nb += n4[d];
+                }
+                sh.prefix = prefix << 8 | (uint32_t)(255 - 4 * tid - last);
+                sh.acc_mass = ml; sh.acc_cnt = nl;
+            }
         }
         __syncthreads();
     }
+    u64 above = sh.acc_mass;
+    if (by == BY_COUNT) {   // the weight in front of the key, which the counts did not need
+        above = 0;
+        for (int i = tid; i < row.V; i += TH) {
+            const float z = row.at(i);
+            if (key_of(z) > sh.prefix) above += w(z);
+        }
+        above = block_reduce(sh, above, [](u64 x, u64 y) { return x + y; });
+    }
     if (tid == 0) {
         const uint32_t ties = sh.cnt[sh.prefix & 255];
-        const u64 each = w(of_key(sh.prefix)), m = sh.acc_mass;
+        const u64 each = w(of_key(sh.prefix)), m = above;
         u64 r = ties;
         if (by == BY_COUNT) r = bound - sh.acc_cnt;
         else if (each) { const u64 lack = by == MASS_AT_LEAST ? bound - m : bound - m + 1; r = (lack + each - 1) / each; }
@@ -143,61 +175,530 @@ __device__ int index_of(Shared &sh, const Row<T> &row, uint32_t key, int rank)
     return sh.hit;
 }
 
+// The row by digits: right for every row, and slow.
 template <typename T>
-__global__ __launch_bounds__(TH) void sample_k(sdlm_sample_args a)
+__device__ void by_digits(Shared &sh, const Row<T> &row, float M, float t, int k, float p, float mp, float u, int *id, float *prob)
+{
+    const Weigh w{(double)M, LOG2E / (double)t};
+    auto add = [](u64 x, u64 y) { return x + y; };
+    u64 n = 0, m = 0, mm = 0;
+    const double least = fmin((double)mp, 1.0) * ONE;
+    for (int i = threadIdx.x; i < row.V; i += TH) {
+        const float z = row.at(i);
+        const u64 x = z == -INFINITY ? 0 : w(z);
+        n += z > -INFINITY; m += x;
+        mm += (double)x >= least ? x : 0;
+    }
+    n = block_reduce(sh, n, add); m = block_reduce(sh, m, add); mm = block_reduce(sh, mm, add);
+    u64 kept = m;
+    if (k > 0 && (u64)k < n) kept = search(sh, row, w, BY_COUNT, (u64)k).mass;
+    if (p < 1.f) kept = search(sh, row, w, MASS_AT_LEAST, (u64)ceil(fmax((double)p, 0.0) * (double)kept)).mass;
+    if (mp > 0.f && mm < kept) kept = mm;
+    const u64 at = (u64)(fmin(fmax((double)u, 0.0), 1.0) * (double)kept);
+    const Found f = search(sh, row, w, MASS_ABOVE, min(at, kept - 1));
+    *id = index_of(sh, row, f.key, f.rank);
+    *prob = (float)((double)w(of_key(f.key)) / (double)kept);
+}
+
+// ------------------------------------------------------------------------------------------------ first launch
+constexpr int PER_THREAD = 64, CHUNK = 256 * PER_THREAD;   // logits of a thread and of a workgroup
+constexpr int RUNS = 9;                        // runs of a thread of the second launch, at most: the largest vocabulary has (524288 + 7) / 64
+constexpr int OCTAVES = 24, PER_OCTAVE = 32, BINS = OCTAVES * PER_OCTAVE, COPIES = 4;   // the last bin, BINS: all below
+constexpr int TOP_MAX = 1024;                  // largest top-k that goes by candidates
+constexpr double Y_MAX = 16384.0;              // largest exponent (of 2) whose fraction keeps 39 bits
+
+// What a row's settings ask of the first launch.
+__device__ inline bool wants_weights(const sdlm_sample_args &a, int r)
+{
+    const float t = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
+    const int k = a.top_k ? a.top_k[r] : 0;
+    return t > 0.f && (k <= 0 || k >= a.vocab) && !(mp > 0.f && !(p < 1.f));
+}
+
+// The row's 16-byte pieces: piece v holds elements [v E - lead, v E - lead + E), E to a piece; lead elements of the first lie in front of the row.
+template <typename T>
+struct Pieces {
+    static constexpr int E = 16 / sizeof(T);
+    const T *z;
+    int V, lead;
+    __device__ Pieces(const sdlm_sample_args &a, int r)
+    {
+        z = (const T *)a.logits + (size_t)r * a.row_stride;
+        V = a.vocab;
+        lead = (int)(((uintptr_t)z & 15) / sizeof(T));
+    }
+    // Elements of piece v; outside the row -infinity, and nothing outside it is read.
+    __device__ void load(int v, float (&x)[E]) const
+    {
+        const int i0 = v * E - lead;
+        if (i0 >= 0 && i0 + E <= V) {
+            const uint4 u = *(const uint4 *)(z + i0);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if constexpr (sizeof(T) == 4) x[e] = canon(__uint_as_float(w[e]));
+                else x[e] = canon(__uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[e] = -INFINITY;
+                if (i0 + e >= 0 && i0 + e < V) x[e] = canon(to_f<T>(z[i0 + e]));
+            }
+        }
+    }
+};
+
+__host__ __device__ inline int n_chunks(int vocab, int esz) { return (vocab + 16 / esz - 1 + CHUNK - 1) / CHUNK; }
+
+// Runs into which a thread's logits are divided, each with a maximum of its own: as many as the second launch can hold, so that also in small vocabularies there are
+// more runs than candidates are asked for.
+template <typename T>
+__host__ __device__ inline int runs_of(int chunks)
+{
+    int n = PER_THREAD * (int)sizeof(T) / 16;
+    while (n > 1 && chunks * n * 256 > TH * RUNS) n >>= 1;
+    return n;
+}
+
+struct SampleWs {
+    uint32_t *top;   // [row][chunk][run of a thread][256]: key of the largest logit of the run
+    int32_t *ref;    // [row][chunk]: the power of two that the chunk's weights are relative to; NONE: no weights
+    u64 *hist;       // [row][chunk][BINS + 1]
+};
+constexpr int NONE = -(1 << 30);
+
+// 2^d in units of 2^-44, d <= 0, to about 2^-31 of itself: a table of 2^(j / 64) and a cubic for the rest.  Only for the sums of bins; the candidates' own weights are exact.
+__device__ inline u64 fast_weight(double d, const double *table)
+{
+    if (d < -46.0) return 0;
+    const double magic = 6755399441055744.0;   // 1.5 2^52: the sum's low bits are the rounded integer
+    const double s = d * 64.0 + magic;
+    const int n = __double2loint(s);
+    const float r = (float)(d - (s - magic) * (1.0 / 64.0)) * 0.69314718056f;   // |r| <= ln 2 / 128
+    const float q = r * (1.f + r * (0.5f + r * 0.16666667f));
+    const double t = table[n & 63];
+    const double w = ldexp(fma(t, (double)q, t), n >> 6);
+    const double m2 = 384.0;                   // 1.5 2^8: an ulp of the sum is 2^-44
+    return (u64)(__double_as_longlong(w + m2) - __double_as_longlong(m2));
+}
+
+__device__ inline int bin_of(double y) { return (int)floor(y * -(double)PER_OCTAVE); }   // absolute: bin - PER_OCTAVE ref counts from the reference
+
+template <typename T>
+__global__ __launch_bounds__(256) void sample_scan_k(sdlm_sample_args a, SampleWs ws, int chunks)
+{
+    constexpr int E = Pieces<T>::E, N = PER_THREAD / E;
+    const int r = blockIdx.x / chunks, c = blockIdx.x % chunks, tid = threadIdx.x;
+    const Pieces<T> row(a, r);
+    const bool weigh = wants_weights(a, r);
+    float x[N][E], top_of[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        row.load(c * (CHUNK / E) + i * 256 + tid, x[i]);
+        top_of[i] = x[i][0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) top_of[i] = fmaxf(top_of[i], x[i][e]);
+    }
+    const int per = runs_of<T>(chunks);
+    uint32_t *keys = ws.top + ((size_t)r * chunks + c) * per * 256 + tid;
+#pragma unroll
+    for (int n = N; n >= 1; n >>= 1) {
+        if (per == n)
+#pragma unroll
+            for (int i = 0; i < n; ++i) keys[i * 256] = key_of(top_of[i]);
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) top_of[i] = fmaxf(top_of[2 * i], top_of[2 * i + 1]);
+    }
+    if (!weigh) return;
+    float mx = top_of[0];
+    __shared__ double table[64];
+    __shared__ u64 hist[COPIES][BINS + 1];
+    __shared__ float red[4];
+    if (tid < 64) table[tid] = exp2(tid * (1.0 / 64.0));
+    for (int i = tid; i < COPIES * (BINS + 1); i += 256) (&hist[0][0])[i] = 0;
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if ((tid & 63) == 0) red[tid >> 6] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const double cs = LOG2E / (double)(a.temperature ? a.temperature[r] : 1.f), top = (double)mx * cs;
+    const bool usable = top > -Y_MAX && top < Y_MAX;
+    const int ref = usable ? (int)ceil(top) : NONE;
+    if (tid == 0) ws.ref[(size_t)r * chunks + c] = ref;
+    if (!usable) return;
+    u64 rest = 0, *mine = hist[tid % COPIES];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const double y = (double)x[i][e] * cs, d = y - ref;
+            if (!(d > -46.0)) continue;
+            const u64 w = fast_weight(d, table);
+            const int b = bin_of(y) + PER_OCTAVE * ref;
+            if (b < BINS) atomicAdd(&mine[max(b, 0)], w);
+            else rest += w;
+        }
+    if (rest) atomicAdd(&mine[BINS], rest);
+    __syncthreads();
+    u64 *out = ws.hist + ((size_t)r * chunks + c) * (BINS + 1);
+    for (int i = tid; i <= BINS; i += 256) {
+        u64 v = 0;
+#pragma unroll
+        for (int k = 0; k < COPIES; ++k) v += hist[k][i];
+        out[i] = v;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ second launch
+constexpr int CAND = 4096;             // candidates that are sorted
+
+struct Lists {
+    u64 cand[CAND];                    // key << 32 | ~index: descending order is the row's order
+    u64 cum[CAND];                     // running weights
+    uint16_t run[TH * RUNS];           // runs that may hold candidates
+    int n_cand, n_run;
+};
+
+// Exclusive prefix sum over the workgroup, and the sum.
+__device__ inline u64 block_scan(Shared &sh, u64 v, u64 *sum)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 x = v;
+    for (int o = 1; o < 64; o <<= 1) { const u64 y = __shfl_up(x, o); if (lane >= o) x += y; }
+    __syncthreads();
+    if (lane == 63) sh.red[wave] = x;
+    __syncthreads();
+    u64 before = 0, s = 0;
+    for (int i = 0; i < TH / 64; ++i) { if (i < wave) before += sh.red[i]; s += sh.red[i]; }
+    *sum = s;
+    return before + x - v;
+}
+
+// The k-th largest of the threads' run maxima (all of them if there are fewer), by digits.
+__device__ uint32_t kth_run(Shared &sh, const uint32_t (&keys)[RUNS], int k)
+{
+    uint32_t prefix = 0;
+    int want = k;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (threadIdx.x < 256) sh.cnt[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < RUNS; ++j)
+            if (keys[j] && (shift == 24 || (keys[j] >> (shift + 8)) == prefix)) atomicAdd(&sh.cnt[(keys[j] >> shift) & 255], 1u);
+        __syncthreads();
+        if (threadIdx.x < 64) {   // lane l: digits 255 - 4 l .. 252 - 4 l
+            const int l = threadIdx.x;
+            int c[4], s = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { c[i] = sh.cnt[255 - 4 * l - i]; s += c[i]; }
+            int x = s;
+            for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o); if (l >= o) x += y; }
+            const u64 reach = __ballot(x >= want);
+            const int at = reach ? __ffsll(reach) - 1 : 63;
+            if (l == at) {
+                int acc = x - s, d = 3;
+                for (int i = 0; i < 4; ++i) if (acc + c[i] >= want) { d = i; break; } else if (i < 3) acc += c[i];
+                sh.prefix = prefix << 8 | (uint32_t)(255 - 4 * l - d);
+                sh.hit = want - acc;
+            }
+        }
+        __syncthreads();
+        prefix = sh.prefix;
+        want = sh.hit;
+        __syncthreads();
+    }
+    return prefix;
+}
+
+// Candidates: the logits whose key is at least `lo` and at most `hi` (and, bin >= 0, that fall into this absolute bin), from the runs whose maximum is at least lo.  Returns whether they fit.
+template <typename T>
+__device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[RUNS], int per, uint32_t lo, uint32_t hi, bool check_bin, int bin, double cs)
+{
+    constexpr int E = Pieces<T>::E, N = PER_THREAD / E;
+    const int g = N / per;             // pieces of a run
+    if (threadIdx.x == 0) { ls.n_cand = 0; ls.n_run = 0; }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < RUNS; ++j)
+        if (keys[j] >= lo && keys[j] > KEY_NEG_INF) ls.run[atomicAdd(&ls.n_run, 1)] = (uint16_t)(threadIdx.x + j * TH);
+    __syncthreads();
+    const int pieces = ls.n_run * g;
+    for (int q = threadIdx.x; q < pieces; q += TH) {
+        const int run = ls.run[q / g], v = ((run >> 8) / per * N + (run >> 8) % per * g + q % g) * 256 + (run & 255);
+        float x[E];
+        row.load(v, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t key = key_of(x[e]);
+            if (key < lo || key > hi || key <= KEY_NEG_INF) continue;
+            if (check_bin && bin_of((double)x[e] * cs) != bin) continue;
+            const int at = atomicAdd(&ls.n_cand, 1);
+            if (at < CAND) ls.cand[at] = (u64)key << 32 | (uint32_t)~(uint32_t)(v * E - row.lead + e);
+        }
+    }
+    __syncthreads();
+    return ls.n_cand <= CAND;
+}
+
+// Sort the n candidates in descending order.
+__device__ void sort(Lists &ls, int n)
+{
+    const int tid = threadIdx.x;
+    if (n <= 512) {   // every candidate counts those in front of it
+        u64 v = 0;
+        int rank = 0;
+        if (tid < n) {
+            v = ls.cand[tid];
+            for (int i = 0; i < n; ++i) rank += ls.cand[i] > v;
+        }
+        __syncthreads();
+        if (tid < n) ls.cand[rank] = v;
+        __syncthreads();
+        return;
+    }
+    int p = 1024;
+    while (p < n) p <<= 1;
+    for (int i = n + tid; i < p; i += TH) ls.cand[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= p; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            for (int i = tid; i < p / 2; i += TH) {
+                const int x = 2 * i - (i & (j - 1)), y = x + j;
+                const u64 u = ls.cand[x], v = ls.cand[y];
+                if ((u < v) == ((x & k) == 0)) { ls.cand[x] = v; ls.cand[y] = u; }
+            }
+            __syncthreads();
+        }
+}
+
+// Running weights of the first n candidates (w: of a logit), starting at `base`.
+template <typename W>
+__device__ void weigh(Shared &sh, Lists &ls, int n, u64 base, const W &w)
+{
+    u64 v[CAND / TH], s = 0, all;
+    const int i0 = threadIdx.x * (CAND / TH);
+#pragma unroll
+    for (int j = 0; j < CAND / TH; ++j) {
+        v[j] = i0 + j < n ? w(of_key((uint32_t)(ls.cand[i0 + j] >> 32))) : 0;
+        s += v[j];
+    }
+    u64 at = base + block_scan(sh, s, &all);
+#pragma unroll
+    for (int j = 0; j < CAND / TH; ++j) {
+        at += v[j];
+        if (i0 + j < n) ls.cum[i0 + j] = at;
+    }
+    __syncthreads();
+}
+
+// The first of n candidates whose running weight is at least (above) `bound`; n if there is none.
+__device__ int first_past(const Lists &ls, int n, u64 bound, bool above)
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (above ? ls.cum[mid] > bound : ls.cum[mid] >= bound) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
+__device__ inline int index_at(const Lists &ls, int i) { return (int)~(uint32_t)ls.cand[i]; }
+__device__ inline float logit_at(const Lists &ls, int i) { return of_key((uint32_t)(ls.cand[i] >> 32)); }
+
+struct FromRef {   // weight against a power of two
+    double cs, ref;
+    __device__ u64 operator()(float z) const
+    {
+        const double d = (double)z * cs - ref;
+        return d < -46.0 ? 0ull : (u64)(exp2(d) * ONE + 0.5);
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs ws, int chunks)
 {
     __shared__ Shared sh;
-    const int r = blockIdx.x;
-    const Row<T> row{(const T *)a.logits + (size_t)r * a.row_stride, a.vocab};
-    uint32_t kmax = 0;
-    for (int i = threadIdx.x; i < row.V; i += TH) kmax = max(kmax, key_of(row.at(i)));
+    __shared__ Lists ls;
+    const int r = blockIdx.x, tid = threadIdx.x, per = runs_of<T>(chunks), runs = chunks * per * 256;
+    const Pieces<T> row(a, r);
+    const Row<T> plain{row.z, row.V};
+    uint32_t keys[RUNS], kmax = 0;
+#pragma unroll
+    for (int j = 0; j < RUNS; ++j) {
+        keys[j] = tid + j * TH < runs ? ws.top[(size_t)r * runs + tid + j * TH] : 0;
+        kmax = max(kmax, keys[j]);
+    }
+    const float t = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
+    const int k = a.top_k ? a.top_k[r] : 0;
     kmax = (uint32_t)block_reduce(sh, kmax, [](u64 x, u64 y) { return x > y ? x : y; });
-    const float M = of_key(kmax), t = a.temperature ? a.temperature[r] : 1.f;
+    const float M = of_key(kmax);
     int id = -1;
     float prob = 0.f;
+    bool done = true;
+    const double cs = LOG2E / (double)t, share = fmin(fmax((double)u, 0.0), 1.0);
+    const bool top_k = k > 0 && k < row.V;
     if (M == -INFINITY) {
         // every token is masked
     } else if (!(t > 0.f)) {
-        id = index_of(sh, row, kmax, 1);
+        if ((done = gather(ls, row, keys, per, kmax, kmax, false, 0, 0.0))) {
+            u64 best = 0;
+            for (int i = tid; i < ls.n_cand; i += TH) best = max(best, ls.cand[i]);
+            id = (int)~(uint32_t)block_reduce(sh, best, [](u64 x, u64 y) { return x > y ? x : y; });
+        } else { id = index_of(sh, plain, kmax, 1); done = true; }
         prob = 1.f;
-    } else {
-        const Weigh w{(double)M, 1.4426950408889634 / (double)t};
-        const int k = a.top_k ? a.top_k[r] : 0;
-        const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
-        auto add = [](u64 x, u64 y) { return x + y; };
-        u64 n = 0, m = 0, mm = 0;
-        const double least = fmin((double)mp, 1.0) * ONE;
-        for (int i = threadIdx.x; i < row.V; i += TH) {
-            const float z = row.at(i);
-            const u64 x = z == -INFINITY ? 0 : w(z);
-            n += z > -INFINITY; m += x;
-            mm += (double)x >= least ? x : 0;
+    } else if (top_k || mp > 0.f) {
+        // candidates are a first part of the order that holds everything that can be kept
+        const Weigh w{(double)M, cs};
+        const bool by_min = !top_k;
+        uint32_t lo;
+        double total = 0.0;
+        if (by_min) {
+            const double z = (double)M + (double)t * log(fmin((double)mp, 1.0));
+            lo = M == INFINITY ? kmax : key_of((float)(z - (fabs(z) + fabs((double)M)) * 1e-6 - 1e-30));   // a little below: the weights decide
+            if (p < 1.f) {       // top_p is a share of the whole row
+                const double top = (double)M * cs;
+                done = fabs(top) < Y_MAX - 64.0;
+                if (done) {
+                    const int ref = (int)ceil(top);
+                    u64 m = 0;
+                    for (int i = tid; i < chunks * (BINS + 1); i += TH) {
+                        const int back = ref - ws.ref[(size_t)r * chunks + i / (BINS + 1)];
+                        if (back < 46) m += ws.hist[(size_t)r * chunks * (BINS + 1) + i] >> back;
+                    }
+                    m = block_reduce(sh, m, [](u64 x, u64 y) { return x + y; });
+                    total = (double)m * exp2((double)ref - top);   // relative to the largest weight, as the candidates' are
+                }
+            }
+        } else {
+            done = k <= TOP_MAX;
+            lo = done ? kth_run(sh, keys, k) : 0;
         }
-        n = block_reduce(sh, n, add); m = block_reduce(sh, m, add); mm = block_reduce(sh, mm, add);
-        u64 kept = m;
-        if (k > 0 && (u64)k < n) kept = search(sh, row, w, BY_COUNT, (u64)k).mass;
-        if (p < 1.f) kept = search(sh, row, w, MASS_AT_LEAST, (u64)ceil(fmax((double)p, 0.0) * (double)kept)).mass;
-        if (mp > 0.f && mm < kept) kept = mm;
-        const float u = a.u[r];
-        const u64 at = (u64)(fmin(fmax((double)u, 0.0), 1.0) * (double)kept);
-        const Found f = search(sh, row, w, MASS_ABOVE, min(at, kept - 1));
-        id = index_of(sh, row, f.key, f.rank);
-        prob = (float)((double)w(of_key(f.key)) / (double)kept);
+        done = done && gather(ls, row, keys, per, lo, 0xffffffffu, false, 0, 0.0);
+        if (done) {
+            int n = ls.n_cand;
+            sort(ls, n);
+            if (top_k) n = min(n, k);
+            weigh(sh, ls, n, 0, w);
+            if (top_k) total = (double)ls.cum[n - 1];
+            int keep = n;
+            if (p < 1.f) keep = min(n, 1 + first_past(ls, n, (u64)fmin(ceil(fmax((double)p, 0.0) * total), 1.8e19), false));
+            if (mp > 0.f) {   // weights fall along the order: the first that is too light ends it
+                const double least = fmin((double)mp, 1.0) * ONE;
+                int l = 1, h = keep;
+                while (l < h) {
+                    const int mid = (l + h) >> 1;
+                    if ((double)(ls.cum[mid] - ls.cum[mid - 1]) < least) h = mid; else l = mid + 1;
+                }
+                keep = h;
+            }
+            const u64 kept = ls.cum[keep - 1];
+            const int at = first_past(ls, keep, min((u64)(share * (double)kept), kept - 1), true);
+            id = index_at(ls, at);
+            prob = (float)((double)(ls.cum[at] - (at ? ls.cum[at - 1] : 0)) / (double)kept);
+        }
+    } else {
+        // the whole row, by the histogram
+        const double top = (double)M * cs;
+        done = fabs(top) < Y_MAX - 64.0;
+        if (done) {
+            const int ref = (int)ceil(top);
+            const FromRef w{cs, (double)ref};
+            u64 m = 0, rest = 0, all, rest_all;
+            if (tid < BINS)
+                for (int c = 0; c < chunks; ++c) {
+                    const int back = ref - ws.ref[(size_t)r * chunks + c], b = tid - PER_OCTAVE * back;
+                    if (back >= 46) continue;
+                    if (b >= 0) m += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + b] >> back;
+                    for (int o = tid + BINS - PER_OCTAVE * back; back > 0 && o < BINS; o += BINS) if (o >= 0) rest += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + o] >> back;
+                    if (tid == 0) rest += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + BINS] >> back;
+                }
+            const u64 before = block_scan(sh, m, &all);
+            block_scan(sh, rest, &rest_all);
+            const u64 total = all + rest_all;
+            // The bin in which the running weight passes `bound`, its sorted candidates and their running weights; the place of the one that passes it, or -1.
+            auto locate = [&](u64 bound, bool above) -> int {
+                if (tid == 0) sh.hit = -1;
+                __syncthreads();
+                const u64 end = before + m;
+                if (tid < BINS && m && (above ? end > bound && before <= bound : end >= bound && before < bound)) { sh.hit = tid; sh.acc_mass = before; }
+                __syncthreads();
+                const int b = sh.hit;
+                const u64 base = sh.acc_mass;
+                __syncthreads();
+                if (b < 0) return -1;      // among the lightest
+                const int bin = b - PER_OCTAVE * ref;
+                // logits of the bin, a little widened: -bin / PER_OCTAVE >= y > -(bin + 1) / PER_OCTAVE
+                const double zh = -(double)bin / PER_OCTAVE / cs, zl = -(double)(bin + 1) / PER_OCTAVE / cs, wide = (fabs(zh) + fabs(zl)) * 1e-6 + 1e-30;
+                if (!gather(ls, row, keys, per, key_of((float)(zl - wide)), key_of((float)(zh + wide)), true, bin, cs) || ls.n_cand == 0) return -1;
+                const int n = ls.n_cand;
+                sort(ls, n);
+                weigh(sh, ls, n, base, w);
+                return min(first_past(ls, n, bound, above), n - 1);   // the bin's sum is rounded otherwise than its parts: at most the last
+            };
+            u64 kept = total;
+            if (p < 1.f) {
+                const u64 bound = max((u64)ceil(fmax((double)p, 0.0) * (double)total), (u64)1);
+                const int at = locate(bound, false);
+                done = at >= 0;
+                if (done) kept = ls.cum[at];
+                __syncthreads();
+            }
+            if (done) {
+                const int at = locate(min((u64)(share * (double)kept), kept - 1), true);
+                done = at >= 0;
+                if (done) {
+                    id = index_at(ls, at);
+                    prob = (float)((double)w(logit_at(ls, at)) / (double)kept);
+                }
+            }
+        }
     }
-    if (threadIdx.x == 0) {
+    if (!done) {
+        __syncthreads();
+        by_digits(sh, plain, M, t, k, p, mp, u, &id, &prob);
+    }
+    if (tid == 0) {
         a.ids[r] = id;
         if (a.prob) a.prob[r] = prob;
     }
 }
 
+SampleWs sample_ws(int rows, int vocab, void *workspace, size_t *bytes)
+{
+    const size_t n = (size_t)rows * n_chunks(vocab, 2);   // bf16 rows may begin further in front
+    char *w = (char *)workspace;
+    SampleWs s;
+    size_t o = 0;
+    auto take = [&](size_t b) { char *at = w + o; o += (b + 255) / 256 * 256; return at; };
+    s.top = (uint32_t *)take((size_t)rows * TH * RUNS * 4);
+    s.ref = (int32_t *)take(n * 4);
+    s.hist = (u64 *)take(n * (BINS + 1) * 8);
+    *bytes = o;
+    return s;
+}
+
+template <typename T>
+void sample_t(hipStream_t s, const sdlm_sample_args &a, const SampleWs &ws)
+{
+    const int chunks = n_chunks(a.vocab, sizeof(T));
+    hipLaunchKernelGGL(sample_scan_k<T>, dim3((unsigned)a.rows * chunks), dim3(256), 0, s, a, ws, chunks);
+    hipLaunchKernelGGL(sample_draw_k<T>, dim3(a.rows), dim3(TH), 0, s, a, ws, chunks);
+}
+
 }  // namespace
 
-size_t sample_workspace_bytes(int rows, int vocab) { return 256; }
+size_t sample_workspace_bytes(int rows, int vocab)
+{
+    size_t n;
+    sample_ws(rows > 0 ? rows : 1, vocab, nullptr, &n);
+    return n;
+}
 
 void launch_sample(hipStream_t s, const sdlm_sample_args &a, void *workspace)
 {
-    if (a.dtype == 0) hipLaunchKernelGGL(sample_k<float>, dim3(a.rows), dim3(TH), 0, s, a);
-    else hipLaunchKernelGGL(sample_k<bf16_t>, dim3(a.rows), dim3(TH), 0, s, a);
+    size_t n;
+    const SampleWs ws = sample_ws(a.rows, a.vocab, workspace, &n);
+    if (a.dtype == 0) sample_t<float>(s, a, ws); else sample_t<bf16_t>(s, a, ws);
 }
 
 }  // namespace sdlm
