@@ -55,10 +55,11 @@ struct Weigh {
 struct Found { uint32_t key; int rank; u64 mass; };
 
 struct Shared {
-    u64 mass[256];
-    uint32_t cnt[256];
+    u64 mass[2048];
+    uint32_t cnt[2048];
     u64 red[TH / 64];
     Found f;
+    u64 w;
     uint32_t prefix;
     u64 acc_mass, acc_cnt;
     int hit;
@@ -84,22 +85,23 @@ __device__ Found search(Shared &sh, const Row<T> &row, const Weigh &w, int by, u
 {
     const int tid = threadIdx.x;
     if (tid == 0) { sh.prefix = 0; sh.acc_mass = 0; sh.acc_cnt = 0; }
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) { sh.mass[tid] = 0; sh.cnt[tid] = 0; }
+    for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {   // digits of 11, 11 and 10 bits: wide ones, so that the lanes of a wavefront seldom meet in one
+        const int bits = shift == 0 ? 10 : 11, digits = 1 << bits, per = digits / 64;
+        for (int i = tid; i < digits; i += TH) { sh.mass[i] = 0; sh.cnt[i] = 0; }
         __syncthreads();
         const uint32_t prefix = sh.prefix;
         for (int i = tid; i < row.V; i += TH) {
             const float z = row.at(i);
             const uint32_t k = key_of(z);
-            if (z == -INFINITY || (shift < 24 && (k >> (shift + 8)) != prefix)) continue;
-            atomicAdd(&sh.cnt[(k >> shift) & 255], 1u);
-            if (by != BY_COUNT) atomicAdd(&sh.mass[(k >> shift) & 255], w(z));
+            if (z == -INFINITY || (shift < 21 && (k >> (shift + bits)) != prefix)) continue;
+            atomicAdd(&sh.cnt[(k >> shift) & (digits - 1)], 1u);
+            if (by != BY_COUNT) atomicAdd(&sh.mass[(k >> shift) & (digits - 1)], w(z));
         }
         __syncthreads();
-        if (tid < 64) {   // lane l: digits 255 - 4 l .. 252 - 4 l
-            u64 m4[4], n4[4], m = 0, n = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { m4[i] = sh.mass[255 - 4 * tid - i]; n4[i] = sh.cnt[255 - 4 * tid - i]; m += m4[i]; n += n4[i]; }
+        if (tid < 64) {   // lane l: `per` digits, from the highest down
+            const int top = digits - 1 - per * tid;
+            u64 m = 0, n = 0;
+            for (int i = 0; i < per; ++i) { m += sh.mass[top - i]; n += sh.cnt[top - i]; }
             u64 ms = m, ns = n;
             for (int o = 1; o < 64; o <<= 1) {
                 const u64 x = __shfl_up(ms, o), y = __shfl_up(ns, o);
@@ -110,18 +112,15 @@ __device__ Found search(Shared &sh, const Row<T> &row, const Weigh &w, int by, u
             u64 lanes = __ballot(n && past(ms, ns));
             if (!lanes) lanes = 1ull << (63 - __clzll((long long)__ballot(n != 0)));   // not passed: the last token
             if (tid == __ffsll(lanes) - 1) {
-                u64 mb = ms - m, nb = ns - n;
+                u64 mb = ms - m, nb = ns - n, ml = mb, nl = nb;
                 int last = 0;
-                u64 ml = mb, nl = nb;
-                bool found = false;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    if (found || !n4[d]) continue;
-                    last = d; ml = mb; nl = nb;
-                    found = past(mb + m4[d], nb + n4[d]);
-                    mb += m4[d]; nb += n4[d];
+                for (int i = 0; i < per; ++i) {
+                    if (!sh.cnt[top - i]) continue;
+                    last = i; ml = mb; nl = nb;
+                    mb += sh.mass[top - i]; nb += sh.cnt[top - i];
+                    if (past(mb, nb)) break;
                 }
-                sh.prefix = prefix << 8 | (uint32_t)(255 - 4 * tid - last);
+                sh.prefix = prefix << bits | (uint32_t)(top - last);
                 sh.acc_mass = ml; sh.acc_cnt = nl;
             }
         }
@@ -137,7 +136,7 @@ __device__ Found search(Shared &sh, const Row<T> &row, const Weigh &w, int by, u
         above = block_reduce(sh, above, [](u64 x, u64 y) { return x + y; });
     }
     if (tid == 0) {
-        const uint32_t ties = sh.cnt[sh.prefix & 255];
+        const uint32_t ties = sh.cnt[sh.prefix & 1023];
         const u64 each = w(of_key(sh.prefix)), m = above;
         u64 r = ties;
         if (by == BY_COUNT) r = bound - sh.acc_cnt;
@@ -214,6 +213,9 @@ __device__ inline bool wants_weights(const sdlm_sample_args &a, int r)
     const int k = a.top_k ? a.top_k[r] : 0;
     return t > 0.f && (k <= 0 || k >= a.vocab) && !(mp > 0.f && !(p < 1.f));
 }
+
+// ... of which min-p needs the sum alone.
+__device__ inline bool wants_sum(const sdlm_sample_args &a, int r) { return a.min_p && a.min_p[r] > 0.f; }
 
 // The row's 16-byte pieces: piece v holds elements [v E - lead, v E - lead + E), E to a piece; lead elements of the first lie in front of the row.
 template <typename T>
@@ -315,6 +317,7 @@ __global__ __launch_bounds__(256) void sample_scan_k(sdlm_sample_args a, SampleW
     __shared__ double table[64];
     __shared__ u64 hist[COPIES][BINS + 1];
     __shared__ float red[4];
+    const bool sum = wants_sum(a, r);
     if (tid < 64) table[tid] = exp2(tid * (1.0 / 64.0));
     for (int i = tid; i < COPIES * (BINS + 1); i += 256) (&hist[0][0])[i] = 0;
     for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
@@ -334,14 +337,14 @@ __global__ __launch_bounds__(256) void sample_scan_k(sdlm_sample_args a, SampleW
             const double y = (double)x[i][e] * cs, d = y - ref;
             if (!(d > -46.0)) continue;
             const u64 w = fast_weight(d, table);
-            const int b = bin_of(y) + PER_OCTAVE * ref;
+            const int b = sum ? BINS : bin_of(y) + PER_OCTAVE * ref;
             if (b < BINS) atomicAdd(&mine[max(b, 0)], w);
             else rest += w;
         }
     if (rest) atomicAdd(&mine[BINS], rest);
     __syncthreads();
     u64 *out = ws.hist + ((size_t)r * chunks + c) * (BINS + 1);
-    for (int i = tid; i <= BINS; i += 256) {
+    for (int i = sum ? BINS + tid : tid; i <= BINS; i += 256) {
         u64 v = 0;
 #pragma unroll
         for (int k = 0; k < COPIES; ++k) v += hist[k][i];
@@ -354,9 +357,12 @@ constexpr int CAND = 4096;             // candidates that are sorted
 
 struct Lists {
     u64 cand[CAND];                    // key << 32 | ~index: descending order is the row's order
-    u64 cum[CAND];                     // running weights
+    u64 cum[CAND];                     // weights, running or single
+    u64 part[TH];                      // the candidates of one fine bin
+    u64 mass[TH];                      // fine bins: weights and counts
+    uint32_t cnt[TH];
     uint16_t run[TH * RUNS];           // runs that may hold candidates
-    int n_cand, n_run;
+    int n_cand, n_run, n_part;
 };
 
 // Exclusive prefix sum over the workgroup, and the sum.
@@ -440,32 +446,32 @@ __device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[R
     return ls.n_cand <= CAND;
 }
 
-// Sort the n candidates in descending order.
-__device__ void sort(Lists &ls, int n)
+// Sort n entries in descending order; with room up to the next power of two.
+__device__ void sort(u64 *v, int n)
 {
     const int tid = threadIdx.x;
-    if (n <= 512) {   // every candidate counts those in front of it
-        u64 v = 0;
+    if (n <= 128) {   // every entry counts those in front of it
+        u64 x = 0;
         int rank = 0;
         if (tid < n) {
-            v = ls.cand[tid];
-            for (int i = 0; i < n; ++i) rank += ls.cand[i] > v;
+            x = v[tid];
+            for (int i = 0; i < n; ++i) rank += v[i] > x;
         }
         __syncthreads();
-        if (tid < n) ls.cand[rank] = v;
+        if (tid < n) v[rank] = x;
         __syncthreads();
         return;
     }
-    int p = 1024;
+    int p = 256;
     while (p < n) p <<= 1;
-    for (int i = n + tid; i < p; i += TH) ls.cand[i] = 0;
+    for (int i = n + tid; i < p; i += TH) v[i] = 0;
     __syncthreads();
     for (int k = 2; k <= p; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
             for (int i = tid; i < p / 2; i += TH) {
                 const int x = 2 * i - (i & (j - 1)), y = x + j;
-                const u64 u = ls.cand[x], v = ls.cand[y];
-                if ((u < v) == ((x & k) == 0)) { ls.cand[x] = v; ls.cand[y] = u; }
+                const u64 f = v[x], g = v[y];
+                if ((f < g) == ((x & k) == 0)) { v[x] = g; v[y] = f; }
             }
             __syncthreads();
         }
@@ -514,6 +520,82 @@ struct FromRef {   // weight against a power of two
     }
 };
 
+// Many candidates are not sorted: they go into TH bins by their key, a thread a bin, and only the bin in which a bound is passed is (4000 candidates: 8 us a bound instead of 30 for
+// all).  base: weight in front of the first candidate.
+struct Picked { u64 mass, w; int index; };   // weight up to and with the candidate, its own, its place in the row
+
+template <typename W>
+struct Fine {
+    Shared &sh;
+    Lists &ls;
+    const W &w;
+    int n, shift;
+    uint32_t hi;
+    u64 m, m_before;
+    int c, c_before;
+    __device__ int bin(u64 cand) const { return (int)((hi - (uint32_t)(cand >> 32)) >> shift); }
+    __device__ Fine(Shared &sh_, Lists &ls_, const W &w_, int n_, u64 base) : sh(sh_), ls(ls_), w(w_), n(n_)
+    {
+        const int tid = threadIdx.x;
+        uint32_t h = 0, l = 0xffffffffu;
+        for (int i = tid; i < n; i += TH) { const uint32_t k = (uint32_t)(ls.cand[i] >> 32); h = max(h, k); l = min(l, k); }
+        hi = (uint32_t)block_reduce(sh, h, [](u64 x, u64 y) { return x > y ? x : y; });
+        const uint32_t lo = (uint32_t)block_reduce(sh, l, [](u64 x, u64 y) { return x < y ? x : y; });
+        const int bits = 32 - __clz((int)(hi - lo));
+        shift = bits > 10 ? bits - 10 : 0;
+        ls.mass[tid] = 0; ls.cnt[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += TH) {
+            const u64 v = ls.cand[i];
+            atomicAdd(&ls.mass[bin(v)], w(of_key((uint32_t)(v >> 32))));
+            atomicAdd(&ls.cnt[bin(v)], 1u);
+        }
+        __syncthreads();
+        u64 all;
+        m = ls.mass[tid]; c = (int)ls.cnt[tid];
+        m_before = base + block_scan(sh, m, &all);
+        c_before = (int)block_scan(sh, c, &all);
+    }
+    // The first candidate by which the running count or weight passes `bound` (the last one if none does); false: its bin is too full.
+    __device__ bool pick(int by, u64 bound, Picked *p)
+    {
+        const int tid = threadIdx.x;
+        __syncthreads();
+        if (tid == 0) { sh.hit = -1; ls.n_part = 0; }
+        __syncthreads();
+        const u64 x0 = by == BY_COUNT ? c_before : m_before, x1 = by == BY_COUNT ? c_before + c : m_before + m;
+        auto past = [&](u64 x) { return by == MASS_ABOVE ? x > bound : x >= bound; };
+        if (c && past(x1) && !past(x0)) { sh.hit = tid; sh.acc_mass = m_before; sh.acc_cnt = c_before; }
+        __syncthreads();
+        if (sh.hit < 0) {   // none: the last candidate's bin
+            const int last = (int)block_reduce(sh, c ? tid : 0, [](u64 x, u64 y) { return x > y ? x : y; });
+            if (tid == last) { sh.hit = tid; sh.acc_mass = m_before; sh.acc_cnt = c_before; }
+            __syncthreads();
+        }
+        const int b = sh.hit;
+        for (int i = tid; i < n; i += TH) {
+            const u64 v = ls.cand[i];
+            if (bin(v) != b) continue;
+            const int at = atomicAdd(&ls.n_part, 1);
+            if (at < TH) ls.part[at] = v;
+        }
+        __syncthreads();
+        const int np = ls.n_part;
+        if (np > TH) return false;
+        sort(ls.part, np);
+        const u64 v = tid < np ? ls.part[tid] : 0, x = tid < np ? w(of_key((uint32_t)(v >> 32))) : 0;
+        u64 all;
+        const u64 before = sh.acc_mass + block_scan(sh, x, &all), seen = sh.acc_cnt + tid;
+        const bool first = by == BY_COUNT ? seen + 1 == bound : past(before + x) && !past(before);
+        const u64 any = __syncthreads_or(tid < np && first);
+        if (tid < np && (any ? first : tid == np - 1)) { sh.f.mass = before + x; sh.w = x; sh.f.rank = (int)~(uint32_t)v; }
+        __syncthreads();
+        *p = Picked{sh.f.mass, sh.w, sh.f.rank};
+        return true;
+    }
+};
+constexpr int SORT_ALL = 128;          // candidates that are simply sorted
+
 template <typename T>
 __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs ws, int chunks)
 {
@@ -561,9 +643,9 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                 if (done) {
                     const int ref = (int)ceil(top);
                     u64 m = 0;
-                    for (int i = tid; i < chunks * (BINS + 1); i += TH) {
-                        const int back = ref - ws.ref[(size_t)r * chunks + i / (BINS + 1)];
-                        if (back < 46) m += ws.hist[(size_t)r * chunks * (BINS + 1) + i] >> back;
+                    for (int c = tid; c < chunks; c += TH) {
+                        const int back = ref - ws.ref[(size_t)r * chunks + c];
+                        if (back < 46) m += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + BINS] >> back;
                     }
                     m = block_reduce(sh, m, [](u64 x, u64 y) { return x + y; });
                     total = (double)m * exp2((double)ref - top);   // relative to the largest weight, as the candidates' are
@@ -576,25 +658,49 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
         done = done && gather(ls, row, keys, per, lo, 0xffffffffu, false, 0, 0.0);
         if (done) {
             int n = ls.n_cand;
-            sort(ls, n);
-            if (top_k) n = min(n, k);
-            weigh(sh, ls, n, 0, w);
-            if (top_k) total = (double)ls.cum[n - 1];
-            int keep = n;
-            if (p < 1.f) keep = min(n, 1 + first_past(ls, n, (u64)fmin(ceil(fmax((double)p, 0.0) * total), 1.8e19), false));
-            if (mp > 0.f) {   // weights fall along the order: the first that is too light ends it
-                const double least = fmin((double)mp, 1.0) * ONE;
-                int l = 1, h = keep;
-                while (l < h) {
-                    const int mid = (l + h) >> 1;
-                    if ((double)(ls.cum[mid] - ls.cum[mid - 1]) < least) h = mid; else l = mid + 1;
+            const double least = fmin((double)mp, 1.0) * ONE;
+            bool fine = n > SORT_ALL;
+            if (fine) {
+                Fine<Weigh> bins(sh, ls, w, n, 0);
+                Picked at;
+                u64 kept = ~0ull, heavy = 0;
+                if (top_k && k < n) { fine = bins.pick(BY_COUNT, (u64)k, &at); kept = at.mass; }
+                else { u64 all; block_scan(sh, bins.m, &all); kept = all; }
+                if (top_k) total = (double)kept;
+                if (fine && p < 1.f) {
+                    const u64 bound = (u64)fmin(ceil(fmax((double)p, 0.0) * total), 1.8e19);
+                    if (bound <= kept) { fine = bins.pick(MASS_AT_LEAST, max(bound, (u64)1), &at); kept = at.mass; }
                 }
-                keep = h;
+                if (fine && mp > 0.f) {
+                    for (int i = tid; i < n; i += TH) { const u64 x = w(logit_at(ls, i)); heavy += (double)x >= least ? x : 0; }
+                    kept = min(kept, block_reduce(sh, heavy, [](u64 x, u64 y) { return x + y; }));
+                }
+                if (fine && (fine = bins.pick(MASS_ABOVE, min((u64)(share * (double)kept), kept - 1), &at))) {
+                    id = at.index;
+                    prob = (float)((double)at.w / (double)kept);
+                }
             }
-            const u64 kept = ls.cum[keep - 1];
-            const int at = first_past(ls, keep, min((u64)(share * (double)kept), kept - 1), true);
-            id = index_at(ls, at);
-            prob = (float)((double)(ls.cum[at] - (at ? ls.cum[at - 1] : 0)) / (double)kept);
+            if (!fine) {
+                __syncthreads();
+                sort(ls.cand, n);
+                if (top_k) n = min(n, k);
+                weigh(sh, ls, n, 0, w);
+                if (top_k) total = (double)ls.cum[n - 1];
+                int keep = n;
+                if (p < 1.f) keep = min(n, 1 + first_past(ls, n, (u64)fmin(ceil(fmax((double)p, 0.0) * total), 1.8e19), false));
+                if (mp > 0.f) {   // weights fall along the order: the first that is too light ends it
+                    int l = 1, h = keep;
+                    while (l < h) {
+                        const int mid = (l + h) >> 1;
+                        if ((double)(ls.cum[mid] - ls.cum[mid - 1]) < least) h = mid; else l = mid + 1;
+                    }
+                    keep = h;
+                }
+                const u64 kept = ls.cum[keep - 1];
+                const int at = first_past(ls, keep, min((u64)(share * (double)kept), kept - 1), true);
+                id = index_at(ls, at);
+                prob = (float)((double)(ls.cum[at] - (at ? ls.cum[at - 1] : 0)) / (double)kept);
+            }
         }
     } else {
         // the whole row, by the histogram
@@ -615,8 +721,8 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             const u64 before = block_scan(sh, m, &all);
             block_scan(sh, rest, &rest_all);
             const u64 total = all + rest_all;
-            // The bin in which the running weight passes `bound`, its sorted candidates and their running weights; the place of the one that passes it, or -1.
-            auto locate = [&](u64 bound, bool above) -> int {
+            // The bin in which the running weight passes `bound`, and the token of it that does.
+            auto locate = [&](u64 bound, bool above, Picked *p) -> bool {
                 if (tid == 0) sh.hit = -1;
                 __syncthreads();
                 const u64 end = before + m;
@@ -625,31 +731,33 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                 const int b = sh.hit;
                 const u64 base = sh.acc_mass;
                 __syncthreads();
-                if (b < 0) return -1;      // among the lightest
+                if (b < 0) return false;   // among the lightest
                 const int bin = b - PER_OCTAVE * ref;
                 // logits of the bin, a little widened: -bin / PER_OCTAVE >= y > -(bin + 1) / PER_OCTAVE
                 const double zh = -(double)bin / PER_OCTAVE / cs, zl = -(double)(bin + 1) / PER_OCTAVE / cs, wide = (fabs(zh) + fabs(zl)) * 1e-6 + 1e-30;
-                if (!gather(ls, row, keys, per, key_of((float)(zl - wide)), key_of((float)(zh + wide)), true, bin, cs) || ls.n_cand == 0) return -1;
+                if (!gather(ls, row, keys, per, key_of((float)(zl - wide)), key_of((float)(zh + wide)), true, bin, cs) || ls.n_cand == 0) return false;
                 const int n = ls.n_cand;
-                sort(ls, n);
+                if (n > SORT_ALL) {
+                    Fine<FromRef> bins(sh, ls, w, n, base);
+                    if (bins.pick(above ? MASS_ABOVE : MASS_AT_LEAST, bound, p)) return true;
+                    __syncthreads();
+                }
+                sort(ls.cand, n);
                 weigh(sh, ls, n, base, w);
-                return min(first_past(ls, n, bound, above), n - 1);   // the bin's sum is rounded otherwise than its parts: at most the last
+                const int at = min(first_past(ls, n, bound, above), n - 1);   // the bin's sum is rounded otherwise than its parts: at most the last
+                *p = Picked{ls.cum[at], w(logit_at(ls, at)), index_at(ls, at)};
+                return true;
             };
             u64 kept = total;
+            Picked at;
             if (p < 1.f) {
-                const u64 bound = max((u64)ceil(fmax((double)p, 0.0) * (double)total), (u64)1);
-                const int at = locate(bound, false);
-                done = at >= 0;
-                if (done) kept = ls.cum[at];
+                done = locate(max((u64)ceil(fmax((double)p, 0.0) * (double)total), (u64)1), false, &at);
+                kept = at.mass;
                 __syncthreads();
             }
-            if (done) {
-                const int at = locate(min((u64)(share * (double)kept), kept - 1), true);
-                done = at >= 0;
-                if (done) {
-                    id = index_at(ls, at);
-                    prob = (float)((double)w(logit_at(ls, at)) / (double)kept);
-                }
+            if (done && (done = locate(min((u64)(share * (double)kept), kept - 1), true, &at))) {
+                id = at.index;
+                prob = (float)((double)at.w / (double)kept);
             }
         }
     }
