@@ -380,40 +380,35 @@ __device__ inline u64 block_scan(Shared &sh, u64 v, u64 *sum)
     return before + x - v;
 }
 
-// The k-th largest of the threads' run maxima (all of them if there are fewer), by digits.
+// A lower bound of the k-th largest run maximum, by its upper 22 bits (0 if there are fewer runs): the few candidates that it lets in besides cost less than the third pass.
 __device__ uint32_t kth_run(Shared &sh, const uint32_t (&keys)[RUNS], int k)
 {
+    const int tid = threadIdx.x;
     uint32_t prefix = 0;
     int want = k;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (threadIdx.x < 256) sh.cnt[threadIdx.x] = 0;
+    for (int shift = 21; shift >= 10; shift -= 11) {
+        for (int i = tid; i < 2048; i += TH) sh.cnt[i] = 0;
+        if (tid == 0) sh.hit = 0;
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < RUNS; ++j)
-            if (keys[j] && (shift == 24 || (keys[j] >> (shift + 8)) == prefix)) atomicAdd(&sh.cnt[(keys[j] >> shift) & 255], 1u);
+            if (keys[j] && (shift == 21 || (keys[j] >> 21) == prefix)) atomicAdd(&sh.cnt[(keys[j] >> shift) & 2047], 1u);
         __syncthreads();
-        if (threadIdx.x < 64) {   // lane l: digits 255 - 4 l .. 252 - 4 l
-            const int l = threadIdx.x;
-            int c[4], s = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { c[i] = sh.cnt[255 - 4 * l - i]; s += c[i]; }
-            int x = s;
-            for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o); if (l >= o) x += y; }
-            const u64 reach = __ballot(x >= want);
-            const int at = reach ? __ffsll(reach) - 1 : 63;
-            if (l == at) {
-                int acc = x - s, d = 3;
-                for (int i = 0; i < 4; ++i) if (acc + c[i] >= want) { d = i; break; } else if (i < 3) acc += c[i];
-                sh.prefix = prefix << 8 | (uint32_t)(255 - 4 * l - d);
-                sh.hit = want - acc;
-            }
+        const int d = 2047 - 2 * tid, c0 = (int)sh.cnt[d], c1 = (int)sh.cnt[d - 1];   // two digits a thread, from the highest down
+        u64 all;
+        const int before = (int)block_scan(sh, c0 + c1, &all);
+        if (before < want && before + c0 + c1 >= want) {
+            const bool first = before + c0 >= want;
+            sh.prefix = (shift == 21 ? 0u : prefix << 11) | (uint32_t)(first ? d : d - 1);
+            sh.hit = want - before - (first ? 0 : c0);
         }
         __syncthreads();
-        prefix = sh.prefix;
         want = sh.hit;
+        if (want == 0) return 0;
+        prefix = sh.prefix;
         __syncthreads();
     }
-    return prefix;
+    return prefix << 10;
 }
 
 // Candidates: the logits whose key is at least `lo` and at most `hi` (and, bin >= 0, that fall into this absolute bin), from the runs whose maximum is at least lo.  Returns whether they fit.
