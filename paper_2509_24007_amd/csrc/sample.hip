@@ -229,24 +229,31 @@ struct Pieces {
         V = a.vocab;
         lead = (int)(((uintptr_t)z & 15) / sizeof(T));
     }
-    // Elements of piece v; outside the row -infinity, and nothing outside it is read.
-    __device__ void load(int v, float (&x)[E]) const
+    // Piece v as it lies in memory; outside the row -infinity, and nothing outside it is read.
+    __device__ uint4 raw(int v) const
     {
         const int i0 = v * E - lead;
-        if (i0 >= 0 && i0 + E <= V) {
-            const uint4 u = *(const uint4 *)(z + i0);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        if (i0 >= 0 && i0 + E <= V) return *(const uint4 *)(z + i0);
+        uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if constexpr (sizeof(T) == 4) x[e] = canon(__uint_as_float(w[e]));
-                else x[e] = canon(__uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16));
-            }
-        } else {
+        for (int k = 0; k < 4; ++k) {
+            w[k] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                x[e] = -INFINITY;
-                if (i0 + e >= 0 && i0 + e < V) x[e] = canon(to_f<T>(z[i0 + e]));
-            }
+            for (int e = k * E / 4; e < (k + 1) * E / 4; ++e)
+                if (i0 + e >= 0 && i0 + e < V) {
+                    if constexpr (sizeof(T) == 4) w[k] = __float_as_uint(z[i0 + e]);
+                    else w[k] = e & 1 ? (w[k] & 0xffffu) | (uint32_t)z[i0 + e] << 16 : (w[k] & 0xffff0000u) | z[i0 + e];
+                }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ void values(const uint4 &u, float (&x)[E])
+    {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if constexpr (sizeof(T) == 4) x[e] = canon(__uint_as_float(w[e]));
+            else x[e] = canon(__uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16));
         }
     }
 };
@@ -297,7 +304,7 @@ __global__ __launch_bounds__(256) void sample_scan_k(sdlm_sample_args a, SampleW
     float x[N][E], top_of[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        row.load(c * (CHUNK / E) + i * 256 + tid, x[i]);
+        row.values(row.raw(c * (CHUNK / E) + i * 256 + tid), x[i]);
         top_of[i] = x[i][0];
 #pragma unroll
         for (int e = 1; e < E; ++e) top_of[i] = fmaxf(top_of[i], x[i][e]);
@@ -416,18 +423,18 @@ template <typename T>
 __device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[RUNS], int per, uint32_t lo, uint32_t hi, bool check_bin, int bin, double cs)
 {
     constexpr int E = Pieces<T>::E, N = PER_THREAD / E;
-    const int g = N / per;             // pieces of a run
+    const int lp = 31 - __clz(per), lg = 31 - __clz(N) - lp;   // log2 of the runs of a thread of the first launch, and of a run's pieces
     if (threadIdx.x == 0) { ls.n_cand = 0; ls.n_run = 0; }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < RUNS; ++j)
         if (keys[j] >= lo && keys[j] > KEY_NEG_INF) ls.run[atomicAdd(&ls.n_run, 1)] = (uint16_t)(threadIdx.x + j * TH);
     __syncthreads();
-    const int pieces = ls.n_run * g;
+    const int pieces = ls.n_run << lg;
     for (int q = threadIdx.x; q < pieces; q += TH) {
-        const int run = ls.run[q / g], v = ((run >> 8) / per * N + (run >> 8) % per * g + q % g) * 256 + (run & 255);
+        const int run = ls.run[q >> lg], v = (((run >> 8) << lg) + (q & ((1 << lg) - 1))) * 256 + (run & 255);
         float x[E];
-        row.load(v, x);
+        row.values(row.raw(v), x);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const uint32_t key = key_of(x[e]);
@@ -705,14 +712,20 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             const int ref = (int)ceil(top);
             const FromRef w{cs, (double)ref};
             u64 m = 0, rest = 0, all, rest_all;
+            for (int c = tid; c < chunks; c += TH) sh.cnt[c] = (uint32_t)min(ref - ws.ref[(size_t)r * chunks + c], 46);   // octaves that a chunk's weights are moved down; 46: all of it
+            __syncthreads();
+            const u64 *hist = ws.hist + (size_t)r * chunks * (BINS + 1);
             if (tid < BINS)
+#pragma unroll 4
                 for (int c = 0; c < chunks; ++c) {
-                    const int back = ref - ws.ref[(size_t)r * chunks + c], b = tid - PER_OCTAVE * back;
-                    if (back >= 46) continue;
-                    if (b >= 0) m += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + b] >> back;
-                    for (int o = tid + BINS - PER_OCTAVE * back; back > 0 && o < BINS; o += BINS) if (o >= 0) rest += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + o] >> back;
-                    if (tid == 0) rest += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + BINS] >> back;
+                    const int back = (int)sh.cnt[c], b = tid - PER_OCTAVE * back;
+                    m += (b >= 0 && back < 46 ? hist[c * (BINS + 1) + b] : 0) >> back;
                 }
+            for (int c = 0; c < chunks; ++c) {   // what falls below the last bin
+                const int back = (int)sh.cnt[c];
+                if (back == 46) continue;
+                for (int o = max(BINS - PER_OCTAVE * back, 0) + tid; o <= BINS; o += TH) rest += hist[c * (BINS + 1) + o] >> back;
+            }
             const u64 before = block_scan(sh, m, &all);
             block_scan(sh, rest, &rest_all);
             const u64 total = all + rest_all;
