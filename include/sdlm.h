@@ -204,6 +204,52 @@ int sdlm_verify_step(sdlm_ctx *ctx, int32_t rule, int32_t *ids_tilde, int32_t *c
 int sdlm_kv_commit(sdlm_ctx *ctx, const int32_t *ids_override, const int32_t *count_override);
 
 /*
+ * Sampled tokens in the place of the arg-max ones: call it between sdlm_decode_step, which wrote `logits` [dev, batch x D x vocab], and sdlm_kv_commit.  Draws a token for every block position
+ * (see sdlm_sample; the vectors are over the batch x D positions), and accepts with the drawn tokens' confidences: the logit confidence is a drawn token's softmax
+ * probability (temperature 1, nothing filtered), the entropy confidence stays the position's.  A position without any token above -infinity keeps its arg-max token.
+ *   ids, count, conf [dev]: as those of the step (conf may be NULL); they replace its result, which a commit without overrides then publishes.
+ * May be repeated.  Asynchronous on the context's stream.  sdlm_verify_step behind it verifies the drawn tokens.  Errors: SDLM_ESTATE without a preceding step, SDLM_EINVAL (also for
+ * vocabularies above 524288).
+ */
+typedef struct {
+    const float *temperature, *top_p, *min_p; /* [dev, batch x D] or NULL: 1, off, off */
+    const int32_t *top_k;                     /* [dev, batch x D] or NULL: off */
+    const float *u;                           /* [dev, batch x D] uniform numbers in [0, 1) */
+} sdlm_sampling;
+int sdlm_sample_step(sdlm_ctx *ctx, const float *logits, const sdlm_sampling *how, int32_t *ids, int32_t *count, float *conf);
+
+/*
+ * Continue sequences as several, drop others: sequence b of the new batch becomes what sequence parents[b] is (`parents` [host], batch entries in 0 .. present batch - 1; batch up to
+ * max_batch).  Several samples of one prompt are one prefill and one fork; a beam's step is a commit and a fork.  Sequences that are nobody's parent are gone, and their pages free.  In the
+ * paged layout full pages are held in common (see sdlm_kv_fork); in the contiguous one a sequence that is no longer alone with its parent takes a free run and a copy of all pages.
+ * The last step's result is discarded.  Synchronises the stream; not under graph capture.
+ * Errors: SDLM_ESTATE before prefill or under capture, SDLM_EINVAL, SDLM_ECAPACITY (too few free pages: nothing was changed).
+ */
+int sdlm_fork(sdlm_ctx *ctx, int32_t batch, const int32_t *parents);
+
+/*
+ * Verify a tree of drafted tokens for every sequence in one pass; call it behind sdlm_decode_step.  Node i of sequence b is token tokens[b * n_nodes + i] behind node parents[b * n_nodes + i] (< i; -1: behind
+ * the known tokens).  A node's prediction is the first token that a block step predicts for the sequence extended by the tokens on the node's branch, the inputs of sdlm_verify_step for every
+ * node at once; the root's is the step's own first arg-max token.  Accepted is the branch that agrees with the predictions: from the root on, the child
+ * whose token is the prediction (the lowest such node), until there is none.
+ *   n_nodes        1 .. 16 D / (D + 1) (D = 1: 1 .. 16); the same for all sequences.  A negative token is no node: fill up with them.
+ *   path           [dev, batch x n_nodes] accepted nodes, then -1; or NULL.
+ *   count, next    [dev, batch] how many, and the prediction behind the last of them; or NULL.
+ *   logits         [dev, batch x n_nodes x vocab] fp32 logits of the nodes' predictions, or NULL.
+ * Reads the cache and writes nothing to it; may be repeated.  A token beyond the vocabulary or a parent that is not in front of its node takes the node out, and sdlm_get_lengths reports it.
+ * Errors: SDLM_ESTATE without a preceding step, SDLM_EINVAL, SDLM_ECAPACITY if the nodes and a block do not fit behind the longest sequence (n + n_nodes + D > max_seq_len), or
+ * batch x n_nodes x (D + 1) rows not into the workspace (sdlm_max_rows; more prefill_rows make room).
+ */
+int sdlm_verify_tree(sdlm_ctx *ctx, int32_t n_nodes, const int32_t *tokens, const int32_t *parents, int32_t *path, int32_t *count, int32_t *next, float *logits);
+
+/*
+ * Publish the accepted branch of the last sdlm_verify_tree, and the prediction behind it: the nodes' K/V are moved into the cache as they are (they were computed under causal attention),
+ * so that only that last token is pending (n_b += count + 1, c_b = n_b - 1).  In the place of sdlm_kv_commit, which publishes the step's own tokens instead.
+ * Errors: SDLM_ESTATE without a preceding sdlm_verify_tree, SDLM_ECAPACITY if the page pool might not hold n_nodes + 1 more tokens of every sequence.
+ */
+int sdlm_tree_commit(sdlm_ctx *ctx);
+
+/*
  * Copy the per-sequence lengths to n [dev, batch] and c [dev, batch] (either may be NULL), then synchronise
  * and refresh the host's bounds.  Returns SDLM_ECAPACITY if a device-side guard (page pool exhausted) or
  * SDLM_EINVAL if a clamped override count was seen since the last call.
@@ -350,6 +396,9 @@ typedef struct {
     int32_t *free_pages;       /* n_pages: the free pages in ascending order, then -1 */
     int32_t *free_count;       /* 1 */
 } sdlm_kv;
+
+/* The cache of a context, to work on it with the operators below in the stream order of the context: lengths are its c.  The memory stays the context's; pages belong to its own calls. */
+int sdlm_kv_describe(sdlm_ctx *ctx, sdlm_kv *kv);
 
 /*
  * Attention of a tree of drafted tokens for each of n_seqs sequences over the cache.  Rows node_offsets[b] .. node_offsets[b+1]-1 of q and out are the nodes of sequence b

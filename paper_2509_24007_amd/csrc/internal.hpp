@@ -113,8 +113,30 @@ struct SeqState {
     int32_t *pend_tok;              // [B][D]: tokens at positions c..n-1
     int32_t *page_table;            // [B][pages_per_seq]
     int32_t *pages_backed;          // [B]
-    int32_t *alloc;                 // [0] next free page, [1] error bits (1: pool exhausted, 2: count clamped, 4: bad override id)
+    int32_t *alloc;                 // [0] pages of free_pages handed out, [1] error bits (1: pool exhausted, 2: count clamped, 4: bad override id), [2] pages in free_pages
+    int32_t *page_refs, *free_pages;// [n_pages]: sequences that hold the page; the free pages, lowest first
     int32_t *last_ids, *last_count; // [B][D], [B]: the last step's result
+    int32_t *arg_ids;               // [B][D]: its arg-max tokens and their confidences, also where a sampled token has replaced them in last_ids
+    float *arg_conf;
+};
+
+// Tokens of a tree that a verification pass takes for a sequence of block size D: with D >= 2 each has a causal row and a block of D rows, and all of them stand in the
+// sequence's D staging tiles.
+__host__ __device__ inline int tree_nodes_max(int D) { return D < 2 ? PAGE : PAGE * D / (D + 1); }
+__host__ __device__ inline int tree_rows_per_node(int D) { return D < 2 ? 1 : D + 1; }
+
+// Device arrays of a tree's verification, per sequence TREE_NODES entries where not said otherwise.
+constexpr int TREE_NODES = 16;
+constexpr int TREE_WORDS = (MAX_D * PAGE + 63) / 64;   // a row's mask over the sequence's staged rows
+struct TreeState {
+    int32_t *path, *path_len, *next;   // accepted nodes, [B] how many, [B] the model's token behind them
+    int32_t *start;                    // [B] where the accepted nodes' K/V go
+    int32_t *ids;                      // predictions of the nodes, T a sequence
+    int32_t *blk_row;                  // the nodes' rows that go through the LM head, T a sequence
+    int32_t *counts;                   // [2][4]: row counts of a full LM-head pass and of the last one
+    int32_t *offsets;                  // [B + 1] first row of a sequence
+    int32_t *tiles;                    // [B][D] staging tiles
+    int64_t *mask;                     // [rows][TREE_WORDS]
 };
 
 struct KvGeom {
@@ -184,7 +206,17 @@ bool lm_accept_applies(int V, int D);
 void launch_lm_accept(hipStream_t s, const float *logits, int V, int conf_fn, const SeqState &st, int B, int D, float tau, int rule, int32_t *ids_out,
                       int32_t *count_out, float *conf_out);
 void launch_commit(hipStream_t s, const SeqState &st, int B, int D, const int32_t *ids_ovr, const int32_t *cnt_ovr,
-                   int paged, int n_pages, int pages_per_seq, int V);
+                   int paged, int pages_per_seq, int V);
+void launch_init_pages(hipStream_t s, const SeqState &st, int used, int n_pages);   // pages 0 .. used-1 are held once, the others free
+// Sequences that continue others (behind launch_fork, unless *status): what else they have of their parents.  old: room for B (D + 2) integers.
+void launch_fork_state(hipStream_t s, const SeqState &st, const int32_t *parent, int n_new, int B, int D, const int32_t *status, int32_t *old);
+// Acceptance of sampled tokens: ids [B][D] replace the step's (-1: the step's own stays).
+void launch_sample_accept(hipStream_t s, const SeqState &st, const int32_t *ids, const float *logits, int V, int B, int D, int conf_fn, float tau, int rule, int32_t *ids_out, int32_t *count_out,
+                          float *conf_out);
+void launch_assemble_tree(hipStream_t s, const SeqState &st, const RowMeta &rm, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int mask_id,
+                          int staging_base, int causal, int V);
+void launch_tree_accept(hipStream_t s, const SeqState &st, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int32_t *path, int32_t *count, int32_t *next);
+void launch_tree_commit(hipStream_t s, const SeqState &st, const TreeState &tr, int B, int D, int paged, int pages_per_seq);
 void launch_read_kv(hipStream_t s, int dtype, const void *pool_layer, const KvGeom &kg, const SeqState &st, int seq,
                     int kvh, int pos0, int count, float *k_out, float *v_out);
 

@@ -1043,7 +1043,7 @@ void launch_lm_reduce(hipStream_t s, const float *logits, int V, int32_t *ids, f
 // The product is a float product taken left to right.  rule 1: leading positions whose own confidence is >= tau.
 // Position j of sequence b: the count is the same in every position's thread, and stored by the first.
 __device__ inline void accept_row(const SeqState &st, const int32_t *ids, const float *conf, int b, int D, int j, float tau, int rule, int32_t *ids_out, int32_t *count_out,
-                                  float *conf_out)
+                                  float *conf_out, bool sampled = false)
 {
     int best = 1;
     if (rule == 0) {
@@ -1059,6 +1059,7 @@ __device__ inline void accept_row(const SeqState &st, const int32_t *ids, const 
     }
     if (j == 0) { st.last_count[b] = best; count_out[b] = best; }
     st.last_ids[b * D + j] = ids[j];
+    if (!sampled) { st.arg_ids[b * D + j] = ids[j]; st.arg_conf[b * D + j] = conf[j]; }
     ids_out[b * D + j] = ids[j];
     if (conf_out) conf_out[b * D + j] = conf[j];
 }
@@ -1148,7 +1149,24 @@ void launch_accept(hipStream_t s, const SeqState &st, const int32_t *ids_rows, c
 // ------------------------------------------------------------------------------------------------ commit
 // c <- n (the pending K/V, already in place, become cache); the accepted tokens become the pending tokens;
 // n <- n + count; the page table grows so that every position < n is backed.
-__global__ void commit_k(SeqState st, int B, int D, const int32_t *ids_ovr, const int32_t *cnt_ovr, int paged, int n_pages,
+// Back n_new positions of sequence b with pages; false (and an error bit): there are none left.
+__device__ inline bool back_positions(const SeqState &st, int b, int n_new, int paged, int pages_per_seq)
+{
+    const int need = (n_new + PAGE - 1) / PAGE - st.pages_backed[b];
+    if (need <= 0) return true;
+    if (!paged || st.pages_backed[b] + need > pages_per_seq) { atomicOr(&st.alloc[1], 1); return false; }
+    const int first = atomicAdd(&st.alloc[0], need);
+    if (first + need > st.alloc[2]) { atomicOr(&st.alloc[1], 1); return false; }
+    for (int i = 0; i < need; ++i) {
+        const int page = st.free_pages[first + i];
+        st.page_refs[page] = 1;
+        st.page_table[(size_t)b * pages_per_seq + st.pages_backed[b] + i] = page;
+    }
+    st.pages_backed[b] += need;
+    return true;
+}
+
+__global__ void commit_k(SeqState st, int B, int D, const int32_t *ids_ovr, const int32_t *cnt_ovr, int paged,
                          int pages_per_seq, int V)
 {
     int b = blockIdx.x * blockDim.x + threadIdx.x;
@@ -1157,14 +1175,7 @@ __global__ void commit_k(SeqState st, int B, int D, const int32_t *ids_ovr, cons
     int cnt = cnt_ovr ? cnt_ovr[b] : st.last_count[b];
     if (cnt < 1 || cnt > D) { atomicOr(&st.alloc[1], 2); cnt = cnt < 1 ? 1 : D; }
     int n = st.n[b], n_new = n + cnt;
-    int need = (n_new + PAGE - 1) / PAGE - st.pages_backed[b];
-    if (need > 0) {
-        if (!paged || st.pages_backed[b] + need > pages_per_seq) { atomicOr(&st.alloc[1], 1); return; }
-        int first = atomicAdd(&st.alloc[0], need);
-        if (first + need > n_pages) { atomicOr(&st.alloc[1], 1); return; }
-        for (int i = 0; i < need; ++i) st.page_table[(size_t)b * pages_per_seq + st.pages_backed[b] + i] = first + i;
-        st.pages_backed[b] += need;
-    }
+    if (!back_positions(st, b, n_new, paged, pages_per_seq)) return;
     for (int i = 0; i < cnt; ++i) {
         int id = ids[i];
         if (id < 0 || id >= V) { atomicOr(&st.alloc[1], 4); id = 0; }   // an override token outside the vocabulary
@@ -1176,9 +1187,175 @@ __global__ void commit_k(SeqState st, int B, int D, const int32_t *ids_ovr, cons
 }
 
 void launch_commit(hipStream_t s, const SeqState &st, int B, int D, const int32_t *ids_ovr, const int32_t *cnt_ovr,
-                   int paged, int n_pages, int pages_per_seq, int V)
+                   int paged, int pages_per_seq, int V)
 {
-    hipLaunchKernelGGL(commit_k, dim3((B + 63) / 64), dim3(64), 0, s, st, B, D, ids_ovr, cnt_ovr, paged, n_pages, pages_per_seq, V);
+    hipLaunchKernelGGL(commit_k, dim3((B + 63) / 64), dim3(64), 0, s, st, B, D, ids_ovr, cnt_ovr, paged, pages_per_seq, V);
+}
+
+__global__ void init_pages_k(SeqState st, int used, int n_pages)
+{
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n_pages; i += gridDim.x * blockDim.x) {
+        st.page_refs[i] = i < used;
+        st.free_pages[i] = i + used < n_pages ? i + used : -1;
+    }
+}
+
+void launch_init_pages(hipStream_t s, const SeqState &st, int used, int n_pages)
+{
+    hipLaunchKernelGGL(init_pages_k, dim3((n_pages + 1023) / 1024 < 64 ? (n_pages + 1023) / 1024 : 64), dim3(256), 0, s, st, used, n_pages);
+}
+
+// ------------------------------------------------------------------------------------------------ forks
+// The fork itself has moved the pages and c; n, the last token and the pending tokens follow here.  One workgroup: the old values are set aside first.
+__global__ __launch_bounds__(1024) void fork_state_k(SeqState st, const int32_t *parent, int n_new, int B, int D, const int32_t *status, int32_t *old)
+{
+    if (*status) return;
+    int32_t *n = old, *last = old + B, *pend = old + 2 * B;
+    for (int i = threadIdx.x; i < B; i += 1024) { n[i] = st.n[i]; last[i] = st.last_tok[i]; }
+    for (int i = threadIdx.x; i < B * D; i += 1024) pend[i] = st.pend_tok[i];
+    __threadfence_block();
+    __syncthreads();
+    for (int b = threadIdx.x; b < n_new; b += 1024) { st.n[b] = n[parent[b]]; st.last_tok[b] = last[parent[b]]; }
+    for (int i = threadIdx.x; i < n_new * D; i += 1024) st.pend_tok[i] = pend[parent[i / D] * D + i % D];
+    if (threadIdx.x == 0) st.alloc[0] = 0;   // the list of free pages is a new one
+}
+
+void launch_fork_state(hipStream_t s, const SeqState &st, const int32_t *parent, int n_new, int B, int D, const int32_t *status, int32_t *old)
+{
+    hipLaunchKernelGGL(fork_state_k, dim3(1), dim3(1024), 0, s, st, parent, n_new, B, D, status, old);
+}
+
+// ------------------------------------------------------------------------------------------------ sampled tokens
+// A sampled token takes the place of the arg-max one.  Its logit confidence is its softmax probability, the arg-max token's times e^(z - z_max); the entropy confidence is of the
+// whole distribution and stays.  One wavefront a sequence, a lane a position.
+__global__ __launch_bounds__(64) void sample_accept_k(SeqState st, const int32_t *ids, const float *logits, int V, int D, int conf_fn, float tau, int rule, int32_t *ids_out, int32_t *count_out,
+                                                      float *conf_out)
+{
+    __shared__ int32_t id_s[MAX_D];
+    __shared__ float conf_s[MAX_D];
+    const int b = blockIdx.x, j = threadIdx.x;
+    if (j < D) {
+        const int arg = st.arg_ids[b * D + j];
+        int id = ids[b * D + j];
+        float c = st.arg_conf[b * D + j];
+        if (id < 0 || id >= V) id = arg;
+        const float *z = logits + ((size_t)b * D + j) * V;
+        if (conf_fn == 0 && id != arg) c *= expf(z[id] - z[arg]);
+        id_s[j] = id;
+        conf_s[j] = c;
+    }
+    __syncthreads();
+    if (j < D) accept_row(st, id_s, conf_s, b, D, j, tau, rule, ids_out, count_out, conf_out, true);
+}
+
+void launch_sample_accept(hipStream_t s, const SeqState &st, const int32_t *ids, const float *logits, int V, int B, int D, int conf_fn, float tau, int rule, int32_t *ids_out, int32_t *count_out,
+                          float *conf_out)
+{
+    hipLaunchKernelGGL(sample_accept_k, dim3(B), dim3(64), 0, s, st, ids, logits, V, D, conf_fn, tau, rule, ids_out, count_out, conf_out);
+}
+
+// ------------------------------------------------------------------------------------------------ trees
+// A node that takes part: its token is in the vocabulary and its parent in front of it.  Others are passed over: they are computed as token 0 behind the root and never accepted.
+__device__ inline bool tree_node(const int32_t *tokens, const int32_t *parents, int i, int V) { return tokens[i] >= 0 && tokens[i] < V && parents[i] >= -1 && parents[i] < i; }
+
+// Rows of the verification of a token tree.  Node i of a sequence with n known tokens, at depth k behind the root (k = 1: a first token), stands for the sequence extended by the
+// tokens on its branch, its own the last:
+//   a causal row at position n + k - 1, which sees the cache [0, n), its ancestors' causal rows and itself;
+//   the block [token, [m] x (D-1)] at positions n + k - 1 .., an ordinary step's block on that longer sequence: it sees the cache, the ancestors' causal rows and itself.
+// With D = 1 the two are one row.  Only the first block row goes through the LM head.  All K/V are staged: row r of a sequence in slot r of its D staging tiles; a row's mask names the slots
+// that it sees.  One workgroup a sequence.
+__global__ __launch_bounds__(64) void assemble_tree_k(SeqState st, RowMeta rm, TreeState tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int mask_id, int stg0,
+                                                      int causal, int V)
+{
+    const int b = blockIdx.x, per = tree_rows_per_node(D), R = T * per, n = st.n[b], tile0 = stg0 + B + b * D;
+    const int32_t *tok = tokens + b * T, *par = parents + b * T;
+    __shared__ uint32_t anc[TREE_NODES];   // strict ancestors of a node
+    __shared__ int depth[TREE_NODES];
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < T; ++i) {
+            const bool ok = tree_node(tok, par, i, V);
+            if (!ok && tok[i] >= 0) atomicOr(&st.alloc[1], 4);
+            const int p = ok ? par[i] : -1;
+            anc[i] = p < 0 ? 0u : anc[p] | 1u << p;
+            depth[i] = p < 0 ? 1 : depth[p] + 1;
+        }
+        if (b == 0) {
+            const int BD = B * D, total = B * T;
+            rm.counts[0] = B * R; rm.counts[1] = 0; rm.counts[2] = 0; rm.counts[3] = 1;
+            tr.counts[0] = B * R; tr.counts[1] = 0; tr.counts[2] = min(BD, total); tr.counts[3] = 1;
+            tr.counts[4] = B * R; tr.counts[5] = 0; tr.counts[6] = total - (total - 1) / BD * BD; tr.counts[7] = 1;
+            tr.offsets[B] = B * R;
+        }
+        tr.offsets[b] = b * R;
+    }
+    for (int j = threadIdx.x; j < D; j += 64) tr.tiles[b * D + j] = tile0 + j;
+    __syncthreads();
+    for (int i = threadIdx.x; i < R; i += 64) {
+        const int node = i < T ? i : (i - T) / D, j = i < T ? 0 : (i - T) % D, r = b * R + i;   // j: row of the block
+        const bool ok = tree_node(tok, par, node, V), block = i >= T;
+        rm.tok[r] = j > 0 ? mask_id : ok ? tok[node] : 0;
+        rm.pos[r] = n + depth[node] - 1 + j;
+        rm.seq[r] = b; rm.kind[r] = i % PAGE; rm.lim[r] = n;
+        rm.stg[r] = tile0 + i / PAGE; rm.smask[r] = 0; rm.stg2[r] = -1;
+        if (block ? j == 0 : D < 2) tr.blk_row[b * T + node] = r;
+        uint64_t w[TREE_WORDS] = {anc[node] | (block ? 0u : 1u << node)};
+        if (block)
+            for (int k = 0; k < (causal ? j + 1 : D); ++k) { const int slot = T + node * D + k; w[slot >> 6] |= 1ull << (slot & 63); }
+        for (int k = 0; k < TREE_WORDS; ++k) tr.mask[(size_t)r * TREE_WORDS + k] = (int64_t)w[k];
+    }
+}
+
+void launch_assemble_tree(hipStream_t s, const SeqState &st, const RowMeta &rm, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int mask_id,
+                          int staging_base, int causal, int V)
+{
+    hipLaunchKernelGGL(assemble_tree_k, dim3(B), dim3(64), 0, s, st, rm, tr, tokens, parents, B, D, T, mask_id, staging_base, causal, V);
+}
+
+// Down the tree from the root: at each point the child whose token is the model's own prediction there (the lowest such node), until there is none.  The root's prediction is the
+// step's first arg-max token, a node's that of its block.
+__global__ void tree_accept_k(SeqState st, TreeState tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int32_t *path, int32_t *count, int32_t *next)
+{
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b >= B) return;
+    const int32_t *tok = tokens + b * T, *par = parents + b * T;
+    int at = -1, y = st.arg_ids[b * D], g = 0;
+    for (int i = 0; i < T; ++i)   // a child stands behind its parent
+        if (par[i] == at && tok[i] == y) {
+            at = i;
+            y = tr.ids[b * T + i];
+            tr.path[b * TREE_NODES + g] = i;
+            if (path) path[b * T + g] = i;
+            ++g;
+        }
+    if (path) for (int i = g; i < T; ++i) path[b * T + i] = -1;
+    tr.path_len[b] = g;
+    tr.next[b] = y;
+    if (count) count[b] = g;
+    if (next) next[b] = y;
+}
+
+void launch_tree_accept(hipStream_t s, const SeqState &st, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int32_t *path, int32_t *count, int32_t *next)
+{
+    hipLaunchKernelGGL(tree_accept_k, dim3((B + 63) / 64), dim3(64), 0, s, st, tr, tokens, parents, B, D, T, path, count, next);
+}
+
+// The accepted nodes become cache (their K/V are moved behind this), the model's token behind them becomes pending.
+__global__ void tree_commit_k(SeqState st, TreeState tr, int B, int D, int paged, int pages_per_seq)
+{
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b >= B) return;
+    const int n = st.n[b], g = tr.path_len[b];
+    tr.start[b] = n;
+    if (!back_positions(st, b, n + g + 1, paged, pages_per_seq)) { tr.path_len[b] = 0; return; }
+    st.pend_tok[b * D] = tr.next[b];
+    st.last_tok[b] = tr.next[b];
+    st.c[b] = n + g;
+    st.n[b] = n + g + 1;
+}
+
+void launch_tree_commit(hipStream_t s, const SeqState &st, const TreeState &tr, int B, int D, int paged, int pages_per_seq)
+{
+    hipLaunchKernelGGL(tree_commit_k, dim3((B + 63) / 64), dim3(64), 0, s, st, tr, B, D, paged, pages_per_seq);
 }
 
 // ------------------------------------------------------------------------------------------------ debug read-back

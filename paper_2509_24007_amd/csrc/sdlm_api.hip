@@ -12,6 +12,7 @@
 
 #include "internal.hpp"
 #include "mfma.hpp"
+#include "ops.hpp"
 
 using namespace sdlm;
 
@@ -63,6 +64,9 @@ struct Layout {
     int verify_rows;
     int group_rows;
     size_t state_ints, meta_ints;
+    size_t page_i32, fork_ws, sample_ws, tree_i32, tree_mask, tree_ws;   // forks, sampled tokens and token trees
+    size_t fork_bytes, tree_ints, tree_ws_bytes;
+    int sample_rows, tree_rows;
     int max_rows, max_groups, pages_per_seq, n_pages, pool_tiles, prefill_rows;
     size_t esz;
     bool mfma;
@@ -138,7 +142,7 @@ void plan(const sdlm_model_cfg *m, const sdlm_run_cfg *r, Layout *L)
     if (L->verify_rows > L->max_rows) L->max_rows = L->verify_rows;
     L->max_rows = (L->max_rows + 63) / 64 * 64;
     L->max_groups = L->max_rows;   // worst case: every row its own group (prefill of many 1-token prompts)
-    L->state_ints = (size_t)B * 3 + (size_t)B * D + (size_t)B * L->pages_per_seq + B + 4 + (size_t)B * D + B;
+    L->state_ints = (size_t)B * 3 + (size_t)B * D + (size_t)B * L->pages_per_seq + B + 4 + (size_t)B * D + B + (size_t)B * D * 2;
     L->state_i32 = take(L->state_ints * 4);
     L->meta_ints = (size_t)L->max_rows * 8 + (size_t)L->max_groups * 6 + (size_t)B * D + 4;
     L->meta_i32 = take(L->meta_ints * 4);
@@ -159,6 +163,21 @@ void plan(const sdlm_model_cfg *m, const sdlm_run_cfg *r, Layout *L)
     L->slabs = take(L->slab_floats * 4);
     L->lm_part = take(L->mfma ? mfma_lm_scratch_bytes(m->vocab, B * D) : 256);
     L->group_rows = L->mfma ? mfma_group_rows(m) : GROUP_ROWS;
+    L->page_i32 = take((size_t)L->n_pages * 2 * 4);
+    sdlm_kv kv = {};
+    kv.max_seqs = B; kv.pages_per_seq = L->pages_per_seq; kv.n_pages = L->n_pages;
+    L->fork_bytes = align_up(fork_workspace_bytes(kv)) + align_up((size_t)B * (D + 3) * 4 + 4);   // behind the fork's own: parents, status, old state
+    L->fork_ws = take(L->fork_bytes);
+    L->sample_rows = B * D < 256 ? B * D : 256;           // rows a launch draws for: beyond, one launch behind the other
+    const size_t sample_bytes = V <= (size_t)SAMPLE_MAX_V ? sample_workspace_bytes(L->sample_rows, m->vocab) : 0;
+    L->sample_ws = take(align_up((size_t)B * D * 4) + sample_bytes);
+    L->tree_rows = B * tree_nodes_max(D) * tree_rows_per_node(D);
+    if (L->tree_rows > L->max_rows) L->tree_rows = L->max_rows;
+    L->tree_ints = (size_t)B * (TREE_NODES * 3 + 3 + 1 + D) + 1 + 8;
+    L->tree_i32 = take(L->tree_ints * 4);
+    L->tree_mask = take((size_t)L->tree_rows * TREE_WORDS * 8);
+    L->tree_ws_bytes = m->dtype == 0 ? 256 : L->mfma ? L->slab_floats * 4 : (size_t)8 << 20;   // matrix-core path: the split-k slabs, free during the attention
+    L->tree_ws = L->mfma ? L->slabs : take(L->tree_ws_bytes);
     L->total = o;
 }
 
@@ -184,7 +203,10 @@ struct sdlm_ctx {
     void *xn, *q, *att, *act, *xhat, *attn_part, *lm_part;
     float *slabs;
     int32_t *ids_rows;
+    TreeState tr;
     int batch = 0;
+    int pages_shared = 0;                // pages that sequences hold in common, counted once less than they are held
+    int tree_nodes = 0;                  // nodes a sequence of the last verify_tree; 0: none since the last step
     int pend_slabs = 0;                  // split-k slabs of the last residual projection not yet added to x
     size_t pend_stride = 0;
     bool prefilled = false, stepped = false;
@@ -262,6 +284,18 @@ bool callers_capture(const sdlm_ctx *c)
     return c->stream && hipStreamIsCapturing(c->stream, &st) == hipSuccess && st != hipStreamCaptureStatusNone;
 }
 
+// The cache as the operators on the caller's tensors know it.  lengths: the context's c, or n for rows that see all known tokens.
+sdlm_kv cache_of(const sdlm_ctx *c, int32_t *lengths)
+{
+    sdlm_kv kv;
+    kv.pool = c->pool; kv.layer_stride = (int64_t)c->kg.layer_stride;
+    kv.n_layers = c->m.n_layers; kv.n_tiles = c->L.pool_tiles; kv.n_kv_heads = c->m.n_kv_heads; kv.head_dim = c->m.head_dim; kv.dtype = c->m.dtype;
+    kv.n_pages = c->L.n_pages; kv.max_seqs = c->r.max_batch; kv.pages_per_seq = c->L.pages_per_seq;
+    kv.page_table = c->st.page_table; kv.lengths = lengths; kv.backed = c->st.pages_backed; kv.page_refs = c->st.page_refs;
+    kv.free_pages = c->st.free_pages; kv.free_count = c->st.alloc + 2;
+    return kv;
+}
+
 // Host upper bound of the longest sequence's length.
 int longest(const sdlm_ctx *c) { return *std::max_element(c->n_ub.begin(), c->n_ub.begin() + c->batch); }
 
@@ -319,8 +353,10 @@ bool step_lm_accept(const sdlm_model_cfg &m, int D) { return !mfma_supported(&m)
 // The decoder layers over the rows described by c->rm.  `rows` bounds the launch grids (the device-side row
 // count decides what is computed); `rows_sure` is a host-known lower bound of that count (it only steers launch shapes).  `max_len`: longest sequence that it may meet (longest, longest_of_step).
 // `cache_only`: the pass only has to leave its rows' K/V in the cache (prefill): the last layer then ends after the K/V placement.  `embedded`: x holds the rows' embeddings already.
+// `tree`: the rows are those of token trees, which see what its masks name.
 // Taps change no product: they copy, add the split-k slabs that the next norm would have added (in the same order), and put operands back into rows.
-void run_layers(sdlm_ctx *c, int rows, int groups, int rows_sure, int max_len, bool cache_only, bool embedded = false, bool two_staging = false)
+void run_layers(sdlm_ctx *c, int rows, int groups, int rows_sure, int max_len, bool cache_only, bool embedded = false, bool two_staging = false,
+                const sdlm_tree_args *tree = nullptr)
 {
     const sdlm_model_cfg &m = c->m;
     const int dt = m.dtype, h = m.hidden, F = m.ffn, d = m.head_dim;
@@ -363,7 +399,8 @@ void run_layers(sdlm_ctx *c, int rows, int groups, int rows_sure, int max_len, b
         bool merge = false;
         {
             Phase p(c, SDLM_PH_ATTN);
-            if (c->L.mfma) merge = launch_attn_mfma(s, &c->m, c->r.max_seq_len, max_len, c->q, c->att, pool_l, c->kg, c->rm, c->st, c->r.block_D, groups, c->attn_part, c->L.attn_bytes, 0, two_staging);
+            if (tree) launch_tree_attention(s, cache_of(c, c->st.n), l, *tree, c->ws + c->L.tree_ws, c->L.tree_ws_bytes);
+            else if (c->L.mfma) merge = launch_attn_mfma(s, &c->m, c->r.max_seq_len, max_len, c->q, c->att, pool_l, c->kg, c->rm, c->st, c->r.block_D, groups, c->attn_part, c->L.attn_bytes, 0, two_staging);
             else launch_attn_generic(s, dt, c->q, c->att, pool_l, c->kg, c->rm, c->st, m.n_q_heads, rows);
         }
         if (merge) {
@@ -455,6 +492,17 @@ int refresh_lengths(sdlm_ctx *c, int32_t *flags_out)
     return SDLM_OK;
 }
 
+// Whether the pool can back `more` further positions of every sequence (paged layout), by the host's bounds, refreshed if need be.
+int pages_suffice(sdlm_ctx *c, int more)
+{
+    if (c->r.kv_layout != 1) return SDLM_OK;
+    auto pages = [&]() { long t = -c->pages_shared; for (int b = 0; b < c->batch; ++b) t += (c->n_ub[b] + more + PAGE - 1) / PAGE; return t; };
+    if (pages() <= c->L.n_pages) return SDLM_OK;
+    const int rc = refresh_lengths(c, nullptr);
+    if (rc) return rc;
+    return pages() > c->L.n_pages ? fail(c, SDLM_ECAPACITY, "page pool (%d pages) would be exhausted", c->L.n_pages) : SDLM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -503,6 +551,14 @@ int sdlm_create(const sdlm_model_cfg *m, const sdlm_run_cfg *r, void *workspace,
     c->st.alloc = si; si += 4;
     c->st.last_ids = si; si += (size_t)B * D;
     c->st.last_count = si; si += B;
+    c->st.arg_ids = si; si += (size_t)B * D;
+    c->st.arg_conf = (float *)si; si += (size_t)B * D;
+    c->st.page_refs = (int32_t *)(ws + L.page_i32); c->st.free_pages = c->st.page_refs + L.n_pages;
+    int32_t *ti = (int32_t *)(ws + L.tree_i32);
+    c->tr.path = ti; ti += (size_t)B * TREE_NODES; c->tr.ids = ti; ti += (size_t)B * TREE_NODES; c->tr.blk_row = ti; ti += (size_t)B * TREE_NODES;
+    c->tr.path_len = ti; ti += B; c->tr.next = ti; ti += B; c->tr.start = ti; ti += B;
+    c->tr.offsets = ti; ti += B + 1; c->tr.tiles = ti; ti += (size_t)B * D; c->tr.counts = ti; ti += 8;
+    c->tr.mask = (int64_t *)(ws + L.tree_mask);
     int32_t *mi = (int32_t *)(ws + L.meta_i32);
     c->rm.tok = mi; mi += L.max_rows; c->rm.pos = mi; mi += L.max_rows; c->rm.seq = mi; mi += L.max_rows;
     c->rm.kind = mi; mi += L.max_rows; c->rm.lim = mi; mi += L.max_rows;
@@ -623,7 +679,7 @@ int sdlm_prefill(sdlm_ctx *c, int32_t batch, const int32_t *ids, const int32_t *
     if (c->r.kv_layout == 1 && pages_needed > c->L.n_pages)
         return fail(c, SDLM_ECAPACITY, "prompts need %ld pages, the pool has %d", pages_needed, c->L.n_pages);
     c->batch = batch;
-    c->prefilled = false; c->stepped = false; c->committed = false;
+    c->prefilled = false; c->stepped = false; c->committed = false; c->tree_nodes = 0; c->pages_shared = 0;
     drop_graph(c);   // the batch size is baked into the captured launches
     // sequence state
     const int B = c->r.max_batch;
@@ -642,7 +698,8 @@ int sdlm_prefill(sdlm_ctx *c, int32_t batch, const int32_t *ids, const int32_t *
             backed[b] = np;
         }
     }
-    int32_t al[4] = {next, 0, 0, 0};
+    const int used = c->r.kv_layout == 0 ? batch * pps : next;
+    int32_t al[4] = {0, 0, c->L.n_pages - used, 0};
     hipStream_t s = c->stream;
     HIPCHK(c, hipMemcpyAsync(c->st.n, n.data(), B * 4, hipMemcpyHostToDevice, s));
     HIPCHK(c, hipMemcpyAsync(c->st.c, n.data(), B * 4, hipMemcpyHostToDevice, s));
@@ -650,6 +707,7 @@ int sdlm_prefill(sdlm_ctx *c, int32_t batch, const int32_t *ids, const int32_t *
     HIPCHK(c, hipMemcpyAsync(c->st.page_table, table.data(), table.size() * 4, hipMemcpyHostToDevice, s));
     HIPCHK(c, hipMemcpyAsync(c->st.pages_backed, backed.data(), B * 4, hipMemcpyHostToDevice, s));
     HIPCHK(c, hipMemcpyAsync(c->st.alloc, al, sizeof al, hipMemcpyHostToDevice, s));
+    launch_init_pages(s, c->st, used, c->L.n_pages);
     HIPCHK(c, hipStreamSynchronize(s));
     // causal passes over the prompts, prefill_rows rows at a time
     const int cap = c->L.prefill_rows;
@@ -759,6 +817,7 @@ static int decode_step_impl(sdlm_ctx *c, int32_t *ids, int32_t *count, float *co
     }
     HIPCHK(c, hipGetLastError());
     c->stepped = true;
+    c->tree_nodes = 0;
     return SDLM_OK;
 }
 
@@ -822,6 +881,7 @@ int sdlm_verify_step(sdlm_ctx *c, int32_t rule, int32_t *ids_tilde, int32_t *cou
         int groups = 0;
         groups = verify_groups_per_seq(D, gr);
         const int cp_floor = c->L.mfma ? mfma_attn_chunk_floor(&c->m, c->r.max_seq_len, B * groups, c->L.attn_bytes) : 0;
+        c->tree_nodes = 0;   // the same staging tiles
         { Phase p(c, SDLM_PH_ROWS); launch_assemble_verify(s, c->st, c->rm, B, D, c->m.mask_token_id, gr, c->kg.staging_base, c->m.block_causal, c->m.n_kv_heads, cp_floor); }
         run_layers(c, rows, B * groups, rows, longest_of_step(c), false, false, !shared);
         run_lm_head(c, B * (D - 1), logits);
@@ -837,20 +897,138 @@ int sdlm_kv_commit(sdlm_ctx *c, const int32_t *ids_override, const int32_t *coun
     if (!c->stepped) return fail(c, SDLM_ESTATE, "kv_commit without a preceding decode_step");
     if ((ids_override == nullptr) != (count_override == nullptr)) return fail(c, SDLM_EINVAL, "pass both overrides or neither");
     const int B = c->batch, D = c->r.block_D;
-    if (c->r.kv_layout == 1) {
-        auto pages = [&]() { long t = 0; for (int b = 0; b < B; ++b) t += (c->n_ub[b] + D + PAGE - 1) / PAGE; return t; };
-        if (pages() > c->L.n_pages) {
-            int rc = refresh_lengths(c, nullptr);
-            if (rc) return rc;
-            if (pages() > c->L.n_pages) return fail(c, SDLM_ECAPACITY, "page pool (%d pages) would be exhausted", c->L.n_pages);
-        }
-    }
-    launch_commit(c->stream, c->st, B, D, ids_override, count_override, c->r.kv_layout, c->L.n_pages, c->L.pages_per_seq, c->m.vocab);
+    int rc = pages_suffice(c, D);
+    if (rc) return rc;
+    launch_commit(c->stream, c->st, B, D, ids_override, count_override, c->r.kv_layout, c->L.pages_per_seq, c->m.vocab);
     HIPCHK(c, hipGetLastError());
     for (int b = 0; b < B; ++b) c->n_ub[b] += D;
     c->commits_unseen |= callers_capture(c);
     c->stepped = false;
+    c->tree_nodes = 0;
     if (!c->committed) { c->committed = true; drop_graph(c); }   // the certain-row bound of the step's launches changes
+    return SDLM_OK;
+}
+
+int sdlm_sample_step(sdlm_ctx *c, const float *logits, const sdlm_sampling *how, int32_t *ids, int32_t *count, float *conf)
+{
+    if (!c) return SDLM_EINVAL;
+    if (!c->stepped) return fail(c, SDLM_ESTATE, "sample_step without a preceding decode_step");
+    if (!logits || !how || !how->u || !ids || !count) return fail(c, SDLM_EINVAL, "logits, the uniform numbers, ids and count are required");
+    if (c->m.vocab > SAMPLE_MAX_V) return fail(c, SDLM_EINVAL, "sample_step takes vocabularies up to %d", SAMPLE_MAX_V);
+    const int R = c->batch * c->r.block_D, V = c->m.vocab;
+    int32_t *drawn = (int32_t *)(c->ws + c->L.sample_ws);
+    void *ws = c->ws + c->L.sample_ws + align_up((size_t)c->r.max_batch * c->r.block_D * 4);
+    for (int r0 = 0; r0 < R; r0 += c->L.sample_rows) {
+        auto at = [&](auto *p) { return p ? p + r0 : p; };
+        sdlm_sample_args a = {};
+        a.logits = logits + (size_t)r0 * V; a.row_stride = V; a.dtype = 0; a.rows = std::min(c->L.sample_rows, R - r0); a.vocab = V;
+        a.temperature = at(how->temperature); a.top_k = at(how->top_k); a.top_p = at(how->top_p); a.min_p = at(how->min_p); a.u = at(how->u);
+        a.ids = drawn + r0;
+        launch_sample(c->stream, a, ws);
+    }
+    launch_sample_accept(c->stream, c->st, drawn, logits, V, c->batch, c->r.block_D, c->r.conf_fn, c->r.tau, c->r.accept_rule, ids, count, conf);
+    HIPCHK(c, hipGetLastError());
+    return SDLM_OK;
+}
+
+int sdlm_fork(sdlm_ctx *c, int32_t batch, const int32_t *parents)
+{
+    if (!c || !parents) return SDLM_EINVAL;
+    if (!c->prefilled) return fail(c, SDLM_ESTATE, "fork before prefill");
+    if (callers_capture(c)) return fail(c, SDLM_ESTATE, "fork synchronises: it cannot be captured");
+    if (batch < 1 || batch > c->r.max_batch) return fail(c, SDLM_EINVAL, "batch %d outside 1..%d", batch, c->r.max_batch);
+    for (int b = 0; b < batch; ++b)
+        if (parents[b] < 0 || parents[b] >= c->batch) return fail(c, SDLM_EINVAL, "parent %d of sequence %d outside 0..%d", parents[b], b, c->batch - 1);
+    const int B = c->r.max_batch, D = c->r.block_D;
+    const sdlm_kv kv = cache_of(c, c->st.c);
+    char *ws = c->ws + c->L.fork_ws;
+    int32_t *par = (int32_t *)(ws + align_up(fork_workspace_bytes(kv))), *status = par + B, *old = status + 1;
+    hipStream_t s = c->stream;
+    HIPCHK(c, hipMemcpyAsync(par, parents, batch * sizeof(int32_t), hipMemcpyHostToDevice, s));
+    launch_fork(s, kv, par, batch, c->r.kv_layout == 1, status, ws);
+    launch_fork_state(s, c->st, par, batch, B, D, status, old);
+    HIPCHK(c, hipGetLastError());
+    int32_t bad = 0, al[3];
+    HIPCHK(c, hipMemcpyAsync(&bad, status, sizeof bad, hipMemcpyDeviceToHost, s));
+    HIPCHK(c, hipMemcpyAsync(al, c->st.alloc, sizeof al, hipMemcpyDeviceToHost, s));
+    HIPCHK(c, hipMemcpyAsync(c->n_host.data(), c->st.n, sizeof(int32_t) * B, hipMemcpyDeviceToHost, s));
+    HIPCHK(c, hipStreamSynchronize(s));
+    if (bad) return fail(c, SDLM_ECAPACITY, "the pool has too few free pages for %d sequences: nothing was changed", batch);
+    c->batch = batch;
+    c->stepped = false;
+    c->tree_nodes = 0;
+    long held = 0;
+    for (int b = 0; b < batch; ++b) { c->n_ub[b] = c->n_host[b]; held += (c->n_host[b] + PAGE - 1) / PAGE; }
+    c->pages_shared = c->r.kv_layout == 1 ? (int)(held - (c->L.n_pages - al[2])) : 0;
+    drop_graph(c);
+    return SDLM_OK;
+}
+
+int sdlm_verify_tree(sdlm_ctx *c, int32_t n_nodes, const int32_t *tokens, const int32_t *parents, int32_t *path, int32_t *count, int32_t *next, float *logits)
+{
+    if (!c) return SDLM_EINVAL;
+    if (!c->stepped) return fail(c, SDLM_ESTATE, "verify_tree without a preceding decode_step");
+    const int B = c->batch, D = c->r.block_D, T = n_nodes, most = tree_nodes_max(D);
+    if (!tokens || !parents) return fail(c, SDLM_EINVAL, "tokens and parents are required");
+    if (T < 1 || T > most) return fail(c, SDLM_EINVAL, "%d nodes: a block size of %d takes 1..%d", T, D, most);
+    const int R = T * tree_rows_per_node(D), rows = B * R;
+    if (rows > c->L.tree_rows) return fail(c, SDLM_ECAPACITY, "%d sequences of %d nodes are %d rows, the workspace has %d (prefill_rows)", B, T, rows, c->L.tree_rows);
+    if (!tree_fits(cache_of(c, c->st.n), c->m.n_q_heads, B, R)) return fail(c, SDLM_ECAPACITY, "%d sequences of up to %d tokens with %d nodes each are too many for one launch", B, c->r.max_seq_len, T);
+    // every node's rows need positions, and a commit may publish T + 1 tokens
+    auto tight = [&]() { for (int b = 0; b < B; ++b) if (c->n_ub[b] + T + D > c->r.max_seq_len) return true; return false; };
+    if (tight()) {
+        const int rc = refresh_lengths(c, nullptr);
+        if (rc) return rc;
+        if (tight()) return fail(c, SDLM_ECAPACITY, "%d nodes and a block of %d behind the longest sequence exceed max_seq_len %d", T, D, c->r.max_seq_len);
+    }
+    hipStream_t s = c->stream;
+    { Phase p(c, SDLM_PH_ROWS); launch_assemble_tree(s, c->st, c->rm, c->tr, tokens, parents, B, D, T, c->m.mask_token_id, c->kg.staging_base, c->m.block_causal, c->m.vocab); }
+    sdlm_tree_args t = {};
+    t.q = c->q; t.out = c->att; t.q_stride = t.out_stride = (int64_t)c->m.n_q_heads * c->m.head_dim;
+    t.n_rows = rows; t.n_seqs = B; t.n_q_heads = c->m.n_q_heads; t.max_nodes = R; t.max_len = longest_of_step(c);
+    t.node_offsets = c->tr.offsets; t.mask = c->tr.mask; t.mask_words = TREE_WORDS; t.node_pages = D; t.node_table = c->tr.tiles;
+    run_layers(c, rows, 0, rows, longest_of_step(c), false, false, false, &t);
+    // the LM head takes batch x D rows at a time
+    const RowMeta rm = c->rm;
+    const int BD = B * D, total = B * T, slabs = c->pend_slabs;
+    for (int r0 = 0; r0 < total; r0 += BD) {
+        const int n = std::min(BD, total - r0);
+        c->rm.blk_row = c->tr.blk_row + r0;
+        c->rm.counts = c->tr.counts + (r0 + BD < total ? 0 : 4);
+        c->pend_slabs = slabs;   // every pass adds the slabs of its own rows
+        run_lm_head(c, n, logits ? logits + (size_t)r0 * c->m.vocab : nullptr);
+        const hipError_t e = hipMemcpyAsync(c->tr.ids + r0, c->ids_rows, n * sizeof(int32_t), hipMemcpyDeviceToDevice, s);
+        if (e != hipSuccess) { c->rm = rm; return fail(c, SDLM_EHIP, "hipMemcpyAsync: %s", hipGetErrorString(e)); }
+    }
+    c->rm = rm;
+    { Phase p(c, SDLM_PH_ACCEPT); launch_tree_accept(s, c->st, c->tr, tokens, parents, B, D, T, path, count, next); }
+    HIPCHK(c, hipGetLastError());
+    c->tree_nodes = T;
+    return SDLM_OK;
+}
+
+int sdlm_tree_commit(sdlm_ctx *c)
+{
+    if (!c) return SDLM_EINVAL;
+    if (!c->stepped || !c->tree_nodes) return fail(c, SDLM_ESTATE, "tree_commit without a preceding verify_tree");
+    const int B = c->batch, D = c->r.block_D, T = c->tree_nodes;
+    const int rc = pages_suffice(c, T + 1);
+    if (rc) return rc;
+    launch_tree_commit(c->stream, c->st, c->tr, B, D, c->r.kv_layout, c->L.pages_per_seq);
+    launch_compact(c->stream, cache_of(c, c->st.c), c->tr.start, c->tr.tiles, D, nullptr, c->tr.path, TREE_NODES, c->tr.path_len, B, T);
+    HIPCHK(c, hipGetLastError());
+    for (int b = 0; b < B; ++b) c->n_ub[b] += T + 1;
+    c->commits_unseen |= callers_capture(c);
+    c->stepped = false;
+    c->tree_nodes = 0;
+    if (!c->committed) { c->committed = true; drop_graph(c); }
+    return SDLM_OK;
+}
+
+int sdlm_kv_describe(sdlm_ctx *c, sdlm_kv *kv)
+{
+    if (!c || !kv) return SDLM_EINVAL;
+    *kv = cache_of(c, c->st.c);
     return SDLM_OK;
 }
 

@@ -546,7 +546,10 @@ void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sd
     m.t = a;
     m.G = t.n_q_heads / kv.n_kv_heads;
     m.c = 1.4426950408889634f / sqrtf((float)kv.head_dim);
-    const Shape sh = shape_of(kv, t.n_q_heads, t.n_seqs, t.max_nodes);
+    Shape sh = shape_of(kv, t.n_q_heads, t.n_seqs, t.max_nodes);
+    // A context lends less workspace than a caller has to: fewer, longer runs.
+    const long fit = (long)((workspace_bytes - 256) / ((size_t)kv.n_kv_heads * 2 * 64 * sh.qt * (kv.head_dim * 4 + 8)));
+    if (fit < sh.groups) sh.groups = fit < 1 ? 1 : (int)fit;
     m.part_o = (float *)workspace;
     m.part_ml = (float2 *)((char *)workspace + (size_t)sh.groups * kv.n_kv_heads * 2 * 64 * sh.qt * kv.head_dim * 4);
     m.groups = sh.groups;

@@ -24,7 +24,8 @@ EXPORTS = ("sdlm_workspace_bytes", "sdlm_create", "sdlm_init_weights", "sdlm_pre
            "sdlm_decode_step_static", "sdlm_graph", "sdlm_verify_step", "sdlm_kv_commit", "sdlm_get_lengths", "sdlm_debug_tap", "sdlm_debug_rows", "sdlm_debug_read_kv",
            "sdlm_debug_gemm_plan", "sdlm_debug_step_plan", "sdlm_max_rows", "sdlm_profile", "sdlm_profile_every", "sdlm_profile_read", "sdlm_kernel_info", "sdlm_last_error",
            "sdlm_destroy", "sdlm_op_error", "sdlm_sample_workspace_bytes", "sdlm_sample", "sdlm_tree_attention_workspace_bytes", "sdlm_tree_attention",
-           "sdlm_kv_fork_workspace_bytes", "sdlm_kv_fork", "sdlm_kv_compact")
+           "sdlm_kv_fork_workspace_bytes", "sdlm_kv_fork", "sdlm_kv_compact", "sdlm_sample_step", "sdlm_fork", "sdlm_verify_tree", "sdlm_tree_commit",
+           "sdlm_kv_describe")
 
 
 class ModelCfg(C.Structure):
@@ -55,6 +56,10 @@ class SampleArgs(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("row_stride", C.c_int64), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32),
                 ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("u", C.c_void_p),
                 ("ids", C.c_void_p), ("prob", C.c_void_p)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("top_k", C.c_void_p), ("u", C.c_void_p)]
 
 
 class KvDesc(C.Structure):
@@ -126,6 +131,16 @@ def load():
     L.sdlm_last_error.argtypes = [vp]
     L.sdlm_destroy.restype = None
     L.sdlm_destroy.argtypes = [vp]
+    L.sdlm_sample_step.restype = C.c_int
+    L.sdlm_sample_step.argtypes = [vp] * 6
+    L.sdlm_fork.restype = C.c_int
+    L.sdlm_fork.argtypes = [vp, i32, vp]
+    L.sdlm_verify_tree.restype = C.c_int
+    L.sdlm_verify_tree.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
+    L.sdlm_tree_commit.restype = C.c_int
+    L.sdlm_tree_commit.argtypes = [vp]
+    L.sdlm_kv_describe.restype = C.c_int
+    L.sdlm_kv_describe.argtypes = [vp, vp]
     L.sdlm_op_error.restype = C.c_char_p
     L.sdlm_op_error.argtypes = []
     L.sdlm_sample_workspace_bytes.restype = sz
@@ -330,6 +345,38 @@ class Context:
             assert ids_override.numel() >= self.batch * self.D and count_override.numel() >= self.batch
             self._order_inputs()
         self._check(self.L.sdlm_kv_commit(self.h, _dp(ids_override), _dp(count_override)))
+
+    # -- sampled tokens, forks, token trees
+    def sample_step(self, logits: torch.Tensor, u: torch.Tensor, ids: torch.Tensor, count: torch.Tensor, conf: Optional[torch.Tensor] = None, *,
+                    temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                    min_p: Optional[torch.Tensor] = None) -> None:
+        """Draw the tokens of the last decode_step, whose `logits` it wrote, instead of taking the arg-max ones (sdlm_sample_step); u and the settings: [batch, D]."""
+        n, f32 = self.batch * self.D, torch.float32
+        how = Sampling(*[_ints(t, n, name, self.device, dt) for t, name, dt in ((temperature, "temperature", f32), (top_p, "top_p", f32), (min_p, "min_p", f32),
+                                                                                (top_k, "top_k", torch.int32), (u, "u", f32))])
+        self._order_inputs()
+        self._check(self.L.sdlm_sample_step(self.h, _ints(logits, n * self.m.vocab, "logits", self.device, f32), C.byref(how), _ints(ids, n, "ids", self.device),
+                                            _ints(count, self.batch, "count", self.device), _ints(conf, n, "conf", self.device, f32)))
+
+    def fork(self, parents: Sequence[int]) -> None:
+        """The new batch's sequence b continues sequence parents[b]; the others end (sdlm_fork).  Synchronises."""
+        p = [int(v) for v in parents]
+        self._check(self.L.sdlm_fork(self.h, len(p), (C.c_int32 * max(1, len(p)))(*p)))
+        self.batch = len(p)
+
+    def verify_tree(self, tokens: torch.Tensor, parents: torch.Tensor, path: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                    next: Optional[torch.Tensor] = None, logits: Optional[torch.Tensor] = None) -> None:
+        """Verify a token tree of every sequence behind the last decode_step (sdlm_verify_tree): tokens, parents, path [batch, nodes], count, next [batch], logits [batch, nodes, vocab]."""
+        if tokens.dim() != 2 or tokens.shape != parents.shape or tokens.shape[0] != self.batch:
+            _refuse("tokens and parents must be [batch, nodes]")
+        B, T = tokens.shape
+        self._order_inputs()
+        self._check(self.L.sdlm_verify_tree(self.h, T, _ints(tokens, B * T, "tokens", self.device), _ints(parents, B * T, "parents", self.device), _ints(path, B * T, "path", self.device),
+                                            _ints(count, B, "count", self.device), _ints(next, B, "next", self.device), _ints(logits, B * T * self.m.vocab, "logits", self.device, torch.float32)))
+
+    def tree_commit(self) -> None:
+        """Publish the branch that the last verify_tree accepted, and the token behind it (sdlm_tree_commit)."""
+        self._check(self.L.sdlm_tree_commit(self.h))
 
     # -- state and debugging
     def get_lengths(self):
