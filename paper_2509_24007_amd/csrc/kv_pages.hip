@@ -159,6 +159,93 @@ __global__ __launch_bounds__(256) void fork_write_k(ForkArgs a)
     if (b == 0 && threadIdx.x == 0) *a.kv.free_count = n_free - need;
 }
 
+// 1 to 4 in one workgroup, for caches whose tables fit LDS: the launches in front of the copies are most of a fork's time (us a fork, 64 sequences of 258 pages 21.8 -> 12.4, 5 of 9 pages 20.6 -> 11.8).
+constexpr int SMALL_TABLE = 20480, SMALL_PAGES = 12288, SMALL_SEQS = 512;
+
+bool fork_small(const sdlm_kv &kv) { return (long)kv.max_seqs * kv.pages_per_seq <= SMALL_TABLE && kv.n_pages <= SMALL_PAGES && kv.max_seqs <= SMALL_SEQS; }
+
+__global__ __launch_bounds__(1024) void fork_small_k(ForkArgs a)
+{
+    __shared__ int32_t table[SMALL_TABLE], refs[SMALL_PAGES];
+    __shared__ int32_t len[SMALL_SEQS], held[SMALL_SEQS], par[SMALL_SEQS], heir[SMALL_SEQS], keep[SMALL_SEQS], first[SMALL_SEQS];
+    __shared__ int bad_s;
+    const int tid = threadIdx.x, S = a.kv.max_seqs, pps = a.kv.pages_per_seq, P = a.kv.n_pages;
+    for (int i = tid; i < S * pps; i += 1024) table[i] = a.kv.page_table[i];
+    for (int i = tid; i < P; i += 1024) refs[i] = 0;
+    if (tid == 0) bad_s = 0;
+    if (tid < S) {
+        const int h = min(max(a.kv.backed[tid], 0), pps), p = tid < a.n_new ? a.parent[tid] : -1;
+        held[tid] = h;
+        len[tid] = min(max(a.kv.lengths[tid], 0), h * PAGE);
+        par[tid] = p;
+        heir[tid] = S;
+    }
+    __syncthreads();
+    const int p = tid < S ? par[tid] : -1;
+    const bool in = p >= 0 && p < S;
+    if (p < -1 || p >= S) bad_s = 2;
+    if (in) atomicMin(&heir[p], tid);   // its first child
+    __syncthreads();
+    int fresh = 0;
+    if (tid < S) {
+        // the parent's own pages stay with it, or, if it ends here, go to the first of its children
+        const bool mine = in && (p < a.n_new && par[p] == p ? tid == p : heir[p] == tid);
+        keep[tid] = !in ? 0 : mine ? held[p] : a.share ? len[p] / PAGE : 0;
+        fresh = in ? held[p] - keep[tid] : 0;
+    }
+    __syncthreads();
+    const int wave = tid >> 6, lane = tid & 63;   // a wavefront a sequence
+    for (int b = wave; b < a.n_new; b += 16) {
+        const int q = par[b];
+        if (q < 0 || q >= S) continue;
+        const int h = held[q], own = keep[b];
+        for (int j = lane; j < h; j += 64) {
+            const int page = table[q * pps + j];
+            if (page < 0 || page >= P) bad_s = 2;
+            else if (j < own) atomicAdd(&refs[page], 1);
+        }
+    }
+    __syncthreads();
+    // free pages: a stretch of them a thread
+    const int per = (P + 1023) / 1024, p0 = min(tid * per, P), p1 = min(p0 + per, P);
+    int mine_free = 0, n_free, need;
+    for (int i = p0; i < p1; ++i) mine_free += refs[i] == 0;
+    int at = block_scan(mine_free, &n_free);
+    const int at_new = block_scan(fresh, &need);
+    if (tid < S) first[tid] = at_new;
+    const int bad = bad_s | (need > n_free ? 1 : 0);
+    if (tid == 0) { a.w.head[0] = bad ? 0 : need; *a.status = bad; }
+    if (bad) return;
+    for (int i = p0; i < p1; ++i) {
+        int r = refs[i];
+        if (r == 0) {
+            if (at < need) { a.w.free_list[at] = i; r = 1; }
+            else a.kv.free_pages[at - need] = i;
+            ++at;
+        }
+        a.kv.page_refs[i] = r;
+    }
+    for (int i = n_free - need + tid; i < P; i += 1024) a.kv.free_pages[i] = -1;
+    if (tid == 0) *a.kv.free_count = n_free - need;
+    __threadfence_block();
+    __syncthreads();
+    for (int b = wave; b < S; b += 16) {
+        const int q = par[b], h = q < 0 ? 0 : held[q], own = keep[b], k0 = first[b] - own, n = q < 0 ? 0 : len[q];
+        for (int j = lane; j < pps; j += 64) {
+            int page = -1;
+            if (j < h) {
+                page = table[q * pps + j];
+                if (j >= own) {
+                    a.w.src[k0 + j] = j * PAGE < n ? page : -1;   // pages behind the end have nothing to copy
+                    page = a.w.free_list[k0 + j];
+                }
+            }
+            a.kv.page_table[b * pps + j] = page;
+        }
+    }
+    if (tid < S) { a.kv.lengths[tid] = in ? len[p] : 0; a.kv.backed[tid] = in ? held[p] : 0; }
+}
+
 // 5: the copies, 16 bytes a thread at a time: unit = one (new page, layer), consecutive in the pool.
 __global__ __launch_bounds__(256) void fork_copy_k(ForkArgs a, int vec_per_page, size_t layer_vecs)
 {
@@ -190,52 +277,62 @@ void launch_fork(hipStream_t s, const sdlm_kv &kv, const int32_t *parent, int n_
     a.w = fork_ws(kv, workspace, &n);
     const size_t esz = kv.dtype == 0 ? 4 : 2;
     const int vec_per_page = (int)((size_t)kv.n_kv_heads * 2 * PAGE * kv.head_dim * esz / 16);
-    hipLaunchKernelGGL(fork_save_k, dim3(512), dim3(256), 0, s, a);
-    if (n_new > 0) hipLaunchKernelGGL(fork_count_k, dim3(n_new), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(fork_plan_k, dim3(1), dim3(1024), 0, s, a);
-    hipLaunchKernelGGL(fork_write_k, dim3(kv.max_seqs), dim3(256), 0, s, a);
-    if (n_new > 0) hipLaunchKernelGGL(fork_copy_k, dim3(2048), dim3(256), 0, s, a, vec_per_page, (size_t)kv.layer_stride * esz / 16);
+    if (fork_small(kv)) hipLaunchKernelGGL(fork_small_k, dim3(1), dim3(1024), 0, s, a);
+    else {
+        hipLaunchKernelGGL(fork_save_k, dim3(512), dim3(256), 0, s, a);
+        if (n_new > 0) hipLaunchKernelGGL(fork_count_k, dim3(n_new), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(fork_plan_k, dim3(1), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL(fork_write_k, dim3(kv.max_seqs), dim3(256), 0, s, a);
+    }
+    const long units = (long)n_new * (share ? 1 : kv.pages_per_seq) * kv.n_layers;   // share: at most the page that is being written has contents
+    if (n_new > 0) hipLaunchKernelGGL(fork_copy_k, dim3(units < 2048 ? units : 2048), dim3(256), 0, s, a, vec_per_page, (size_t)kv.layer_stride * esz / 16);
 }
 
 namespace {
 
 // K/V of the nodes path[b][0 .. g) -> positions start[b] .. start[b] + g - 1 of sequence b.  One workgroup a (sequence, layer, kv head): it reads MOVE positions before it
-// writes any, and a path ascends (path[i] >= i), so the nodes may stand behind the sequence in its own pages.  One thread an element: a slot's elements are pieces of
-// 16 bytes (K) or single ones (V) all over the tile.
-constexpr int MOVE = 16;
+// writes any, and a path ascends (path[i] >= i), so the nodes may stand behind the sequence in its own pages.  A thread an element of a position: K is in pieces of
+// 16 bytes, V in single elements all over the tile.  Bound by its chain of round trips (length, path, tables, elements): one lane a position looks up both places.
+constexpr int MOVE = 8;
 
 template <typename T>
 __global__ __launch_bounds__(256) void compact_k(sdlm_kv kv, const int32_t *start, const int32_t *node_table, int node_pages, const int32_t *node_base, const int32_t *path,
                                                  int path_stride, const int32_t *path_len, int max_path)
 {
-    const int b = blockIdx.y, l = blockIdx.x / kv.n_kv_heads, h = blockIdx.x % kv.n_kv_heads, d = kv.head_dim;
+    const int b = blockIdx.y, l = blockIdx.x / kv.n_kv_heads, h = blockIdx.x % kv.n_kv_heads, d = kv.head_dim, tid = threadIdx.x;
     const int g = min(path_len[b], max_path), s0 = start[b], base = node_base ? node_base[b] : 0;
-    const size_t tile = (size_t)2 * PAGE * d;
     T *pool = (T *)kv.pool + (size_t)l * kv.layer_stride;
-    const int i0 = threadIdx.x;
+    const size_t tile = (size_t)2 * PAGE * d;
+    __shared__ int2 place[2][MOVE];   // [from, to]: page (-1: passed over) and slot
+    const int e = tid < d ? tid : tid - d;
+    const bool k = tid < d, on = tid < 2 * d;
+    auto at = [&](const int2 &p) { return pool + ((size_t)p.x * kv.n_kv_heads + h) * tile + (k ? k_off(p.y, e) : PAGE * d + v_off(p.y, e)); };
     for (int m0 = 0; m0 < g; m0 += MOVE) {
-        const int m = min(MOVE, g - m0), n = m * 2 * d;
-        T v[MOVE];   // 2 d <= 256 elements a position: one each
+        if (tid < MOVE) {
+            int2 from = make_int2(-1, 0), to = from;
+            if (m0 + tid < g) {
+                const int node = path[(size_t)b * path_stride + m0 + tid];
+                const long src = (long)base + node, dst = (long)s0 + m0 + tid;
+                if (node >= 0 && src >= 0 && src / PAGE < node_pages && dst >= 0 && dst / PAGE < kv.pages_per_seq) {
+                    const int a = node_table[(size_t)b * node_pages + src / PAGE], c = kv.page_table[(size_t)b * kv.pages_per_seq + dst / PAGE];
+                    if (a >= 0 && a < kv.n_tiles && c >= 0 && c < kv.n_tiles) { from = make_int2(a, (int)(src % PAGE)); to = make_int2(c, (int)(dst % PAGE)); }
+                }
+            }
+            place[0][tid] = from;
+            place[1][tid] = to;
+        }
+        __syncthreads();
+        T v[MOVE];
+#pragma unroll
         for (int q = 0; q < MOVE; ++q) {
-            if (q >= m || i0 >= 2 * d) break;
-            const int node = path[(size_t)b * path_stride + m0 + q], at = base + node, e = i0 % d;
             v[q] = T(0);
-            if (node < 0 || at < 0 || at / PAGE >= node_pages) continue;
-            const int page = node_table[(size_t)b * node_pages + at / PAGE];
-            if (page < 0 || page >= kv.n_tiles) continue;
-            v[q] = pool[((size_t)page * kv.n_kv_heads + h) * tile + (i0 < d ? k_off(at % PAGE, e) : PAGE * d + v_off(at % PAGE, e))];
+            if (on && place[0][q].x >= 0) v[q] = *at(place[0][q]);
         }
         __syncthreads();
-        for (int q = 0; q < MOVE; ++q) {
-            if (q >= m || i0 >= 2 * d) break;
-            const int node = path[(size_t)b * path_stride + m0 + q], from = base + node, at = s0 + m0 + q, e = i0 % d;
-            if (node < 0 || from < 0 || from / PAGE >= node_pages || at < 0 || at / PAGE >= kv.pages_per_seq) continue;
-            const int src = node_table[(size_t)b * node_pages + from / PAGE], page = kv.page_table[(size_t)b * kv.pages_per_seq + at / PAGE];
-            if (src < 0 || src >= kv.n_tiles || page < 0 || page >= kv.n_tiles) continue;
-            pool[((size_t)page * kv.n_kv_heads + h) * tile + (i0 < d ? k_off(at % PAGE, e) : PAGE * d + v_off(at % PAGE, e))] = v[q];
-        }
-        __syncthreads();
-        (void)n;
+#pragma unroll
+        for (int q = 0; q < MOVE; ++q)
+            if (on && place[1][q].x >= 0) *at(place[1][q]) = v[q];
+        __syncthreads();   // places, and positions that the next nodes may stand behind
     }
 }
 
