@@ -416,7 +416,7 @@ typedef struct {
     int32_t n_rows, n_seqs;      /* n_rows: rows of q and out in all; n_seqs <= kv->max_seqs */
     int32_t n_q_heads;           /* a multiple of n_kv_heads */
     int32_t max_nodes;           /* 1 .. 1024: most nodes of a sequence */
-    int32_t max_len;             /* most positions of the cache a sequence has; 0: what the table can hold.  Steers the launch; longer ones are still read whole */
+    int32_t max_len;             /* most positions of the cache a sequence has; 0: what the table can hold.  Steers the launch (fp32: and so the order of sums); longer ones are still read whole */
     const int32_t *node_offsets; /* [dev, n_seqs + 1] ascending, 0 .. n_rows */
     const int64_t *mask;         /* [dev] n_rows x mask_words */
     int32_t mask_words;          /* >= (max_nodes + 63) / 64 */

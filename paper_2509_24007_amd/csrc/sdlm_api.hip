@@ -176,7 +176,7 @@ void plan(const sdlm_model_cfg *m, const sdlm_run_cfg *r, Layout *L)
     L->tree_ints = (size_t)B * (TREE_NODES * 3 + 3 + 1 + D) + 1 + 8;
     L->tree_i32 = take(L->tree_ints * 4);
     L->tree_mask = take((size_t)L->tree_rows * TREE_WORDS * 8);
-    L->tree_ws_bytes = m->dtype == 0 ? 256 : L->mfma ? L->slab_floats * 4 : (size_t)8 << 20;   // matrix-core path: the split-k slabs, free during the attention
+    L->tree_ws_bytes = L->mfma ? L->slab_floats * 4 : (size_t)8 << 20;   // matrix-core path: the split-k slabs, free during the attention
     L->tree_ws = L->mfma ? L->slabs : take(L->tree_ws_bytes);
     L->total = o;
 }

@@ -3,6 +3,8 @@
 //   out[r, h] = sum_j p_j V[j], p = softmax over the seen keys of q[r, h] . K[j] / sqrt(d); a node that sees no key gets zeros.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ops.hpp"
 
 namespace sdlm {
@@ -16,9 +18,10 @@ struct TreeArgs {
     float scale;
 };
 
-// fp32.  One workgroup a (node, query head).  The seen tiles, the prefix's and then the nodes', go four at a time to each of four wavefronts, which hold a running maximum, sum and output,
+// Small fp32 calls, one launch.  One workgroup a (node, query head).  The seen tiles, the prefix's and then the nodes', go four at a time to each of four wavefronts, which hold a running maximum, sum and output,
 // merged at the end.  Scores: a key a lane, its features in pieces of 16 bytes.  Output: a feature a lane, four slots a load.  Bound by its chain of round trips (page, K, V) over as
-// many trips as a wavefront has; every row reads the cache anew, which the debug mode's sizes allow (5 sequences of up to 300 positions and 40 nodes 13.7 us, with one wavefront a row 62).
+// many trips as a wavefront has; every row reads the cache anew, so it is taken for few rows over short prefixes only, see few_rows (5 sequences of up to 300 positions and 40 nodes
+// 13.7 us, with one wavefront a row 62).
 template <int HD>
 __global__ __launch_bounds__(256) void tree_rows_k(TreeArgs a)
 {
@@ -115,12 +118,12 @@ __global__ __launch_bounds__(256) void tree_rows_k(TreeArgs a)
     }
 }
 
-// ------------------------------------------------------------------------------------------------ matrix-core path (bf16)
+// ------------------------------------------------------------------------------------------------ matrix-core path
 // The queries of a sequence and kv head are its (node, query head) pairs, in blocks of 16 QT for each of four wavefronts; every tile that the workgroup
 // brings to LDS serves the whole block.  A launch has as many workgroups as the chip holds at once, and the tiles of all blocks, one block behind the other, are
 // dealt out to them in equal runs: no unit waits for another at the end, whatever the lengths are.  A workgroup's run may end inside a block; such a part leaves a
 // maximum, a sum and an unnormalised output, and the parts of a block are merged by a second launch.  At most its first and its last part are incomplete, so a
-// workgroup has two places for them.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
+// workgroup has two places for them.  fp32 tiles and operands take the instruction of 16 x 16 x 4, whose operands are neighbours in the tiles as they are.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
@@ -131,6 +134,10 @@ constexpr int MIN_PAIRS = 2;          // fewest pairs of tiles a workgroup takes
 constexpr float RESCALE_GAP = 8.0f;   // log2 units, see the running maximum below
 
 __device__ inline bool finite16(uint32_t x) { return (x & 0x7f80u) != 0x7f80u; }   // of a bf16's bits
+__device__ inline bool finite32(uint32_t x) { return (x & 0x7f800000u) != 0x7f800000u; }
+
+__device__ inline void store4(float *p, const f32x4 &o) { *(f32x4 *)p = o; }
+__device__ inline void store4(bf16_t *p, const f32x4 &o) { *(uint2 *)p = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])); }
 
 struct MfmaArgs {
     TreeArgs t;
@@ -212,10 +219,12 @@ __device__ inline float max3(float a, float b, float c)   // of results of vecto
     return r;
 }
 
-template <int HD, int QT>
+template <typename T, int HD, int QT>
 __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
 {
-    constexpr int QB = 64 * QT, NK = HD / 32, ND = HD / 16, TILE = 2 * PAGE * HD, VEC = HD / 32;   // VEC: 16-byte loads of a thread for a pair of tiles
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int E = 16 / sizeof(T);                                                              // elements in 16 bytes
+    constexpr int QB = 64 * QT, NK = HD / 32, ND = HD / 16, TILE = 2 * PAGE * HD, VEC = HD / (4 * E);   // VEC: 16-byte loads of a thread for a pair of tiles
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), ln = lane & 15, lg = lane >> 4, G = a.G;
     // Workgroups are dealt to the eight dies in turn: each die gets a stretch of neighbouring runs, whose blocks read the same tiles.
     const int per_die = (gridDim.x + 7) / 8, id = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3), hk = id / a.groups;
@@ -224,9 +233,9 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
     const int all = all_pairs(a.t, sums, G, QB), run = run_of(all, a.groups);
     const int end = (int)min((long)all, (long)(id % a.groups + 1) * run);
     int from = (int)min((long)all, (long)(id % a.groups) * run);
-    __shared__ __attribute__((aligned(16))) bf16_t kv[2][2 * TILE];   // two pairs of tiles, each as in the pool
+    __shared__ __attribute__((aligned(16))) T kv[2][2 * TILE];   // two pairs of tiles, each as in the pool
     __shared__ int strange[2][4];   // per wavefront: whether its part of the pair's values has some that are not finite (only where a query may not see all slots)
-    const bf16_t *pool = (const bf16_t *)a.t.pool;
+    const T *pool = (const T *)a.t.pool;
     for (int part = 0; from < end; ++part) {
     const Place pl = place_of(a.t, sums, G, QB, from, false);
     const int b = uniform(pl.b);
@@ -241,19 +250,31 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
     const int32_t *ptab = a.t.kv.page_table + (size_t)b * a.t.kv.pages_per_seq, *ntab = a.t.t.node_table + (size_t)b * a.t.t.node_pages;
     const int node_tile0 = s.base / PAGE - s.prefix_tiles, shift0 = s.prefix_tiles * PAGE + s.base % PAGE;   // tile u >= prefix_tiles: entry u + node_tile0; its slot i is node u 16 + i - shift0
 
-    Op8 qop[QT][NK];
+    // This wavefront's queries, B operands: lane (query ln, group lg) holds features 32 kk + 8 lg .. + 7 of step kk; fp32: features 8 o + 2 lg and the next, a step each.
+    Op8 qop[QT][F32 ? 1 : NK];
+    float qf[QT][F32 ? HD / 4 : 1];
     int mrow[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int qi = q0 + t * 16 + ln;
         const bool ok = qi < QR;
         const int row = s.first + (ok ? qi / G : 0), h = hk * G + (ok ? qi % G : 0);
-        const bf16_t *qp = (const bf16_t *)a.t.t.q + (size_t)row * a.t.t.q_stride + h * HD + lg * 8;
+        const T *qp = (const T *)a.t.t.q + (size_t)row * a.t.t.q_stride + h * HD + lg * (F32 ? 2 : 8);
         mrow[t] = row;
+        if constexpr (F32) {
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-            qop[t][kk].u = make_uint4(0, 0, 0, 0);
-            if (ok) qop[t][kk].u = *(const uint4 *)(qp + kk * 32);
+            for (int o = 0; o < HD / 8; ++o) {
+                float2 x = make_float2(0.f, 0.f);
+                if (ok) x = *(const float2 *)(qp + o * 8);
+                qf[t][2 * o] = x.x;
+                qf[t][2 * o + 1] = x.y;
+            }
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) {
+                qop[t][kk].u = make_uint4(0, 0, 0, 0);
+                if (ok) qop[t][kk].u = *(const uint4 *)(qp + kk * 32);
+            }
         }
     }
     f32x4 O[QT][ND];
@@ -281,52 +302,67 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
             if (pp + 32 < n_pairs) pg_next = pages(pp / 32 + 1);
         }
         const int pA = __builtin_amdgcn_readlane(pg, 2 * (pp & 31)), pB = __builtin_amdgcn_readlane(pg, 2 * (pp & 31) + 1);
-        const bf16_t *tA = pool + ((size_t)max(pA, 0) * a.t.kv.n_kv_heads + hk) * TILE, *tB = pool + ((size_t)max(pB >= 0 ? pB : pA, 0) * a.t.kv.n_kv_heads + hk) * TILE;
+        const T *tA = pool + ((size_t)max(pA, 0) * a.t.kv.n_kv_heads + hk) * TILE, *tB = pool + ((size_t)max(pB >= 0 ? pB : pA, 0) * a.t.kv.n_kv_heads + hk) * TILE;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const bf16_t *t = wave * 64 + 256 * i < TILE / 8 ? tA : tB - TILE;   // a wavefront's part lies in one tile
-            r[i] = *(const u32x4 *)(t + (unsigned)(tid + 256 * i) * 8);
+            const T *t = wave * 64 + 256 * i < TILE / E ? tA : tB - TILE;   // a wavefront's part lies in one tile
+            r[i] = *(const u32x4 *)(t + (unsigned)(tid + 256 * i) * E);
         }
         return (pA >= 0 ? 1 : 0) | (pB >= 0 ? 2 : 0);
     };
     auto is_whole = [&](int pp, int have) { return have == 3 && (u0 + 2 * pp + 2) * PAGE <= s.len; };   // every key of the pair is seen by every query
     auto stash = [&](int buf, const u32x4 (&r)[VEC], int pp, int have) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) *(u32x4 *)(&kv[buf][0] + (size_t)(tid + 256 * i) * 8) = r[i];
+        for (int i = 0; i < VEC; ++i) *(u32x4 *)(&kv[buf][0] + (size_t)(tid + 256 * i) * E) = r[i];
         if (is_whole(pp, have)) return;
         bool any = false;
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-            if ((tid + 256 * i) % (TILE / 8) >= TILE / 16)
+            if ((tid + 256 * i) % (TILE / E) >= TILE / E / 2)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) any |= !finite16(r[i][k]) || !finite16(r[i][k] >> 16);
+                for (int k = 0; k < 4; ++k) any |= F32 ? !finite32(r[i][k]) : !finite16(r[i][k]) || !finite16(r[i][k] >> 16);
         any = __any(any);
         if (lane == 0) strange[buf][wave] = any;
     };
     auto compute = [&](int pp, int buf, int have) {
         if (!active) return;
         const int uA = u0 + 2 * pp;
-        const bf16_t *KA = &kv[buf][0], *KB = KA + TILE;
+        const T *KA = &kv[buf][0], *KB = KA + TILE;
         f32x4 sA[QT], sB[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t) { sA[t] = f32x4{0.f, 0.f, 0.f, 0.f}; sB[t] = sA[t]; }
+        const T *VA = KA + PAGE * HD, *VB = KB + PAGE * HD;
+        Op8 vo[F32 ? 1 : ND];
+        if constexpr (F32) {
+            // keys as rows, features 8 o + {0, 2, 4, 6} and 8 o + {1, 3, 5, 7} as the four columns of a step: a lane's two are neighbours
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-            Op8 ka, kb;
-            ka.u = *(const uint4 *)(KA + (kk * 64 + lane) * 8);
-            kb.u = *(const uint4 *)(KB + (kk * 64 + lane) * 8);
+            for (int o = 0; o < HD / 8; ++o) {
+                const float2 ka = *(const float2 *)(KA + o * 128 + ln * 8 + lg * 2), kb = *(const float2 *)(KB + o * 128 + ln * 8 + lg * 2);
 #pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                sA[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka.v, qop[t][kk].v, sA[t], 0, 0, 0);
-                sB[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb.v, qop[t][kk].v, sB[t], 0, 0, 0);
+                for (int t = 0; t < QT; ++t) {
+                    sA[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.x, qf[t][2 * o], sA[t], 0, 0, 0);
+                    sB[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kb.x, qf[t][2 * o], sB[t], 0, 0, 0);
+                    sA[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.y, qf[t][2 * o + 1], sA[t], 0, 0, 0);
+                    sB[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kb.y, qf[t][2 * o + 1], sB[t], 0, 0, 0);
+                }
             }
-        }
-        const bf16_t *VA = KA + PAGE * HD, *VB = KB + PAGE * HD;
-        Op8 vo[ND];
+        } else {
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {   // requested here, used behind the softmax
-            vo[dt].h[0] = *(const uint2 *)(VA + (dt * 64 + lane) * 4);
-            vo[dt].h[1] = *(const uint2 *)(VB + (dt * 64 + lane) * 4);
+            for (int kk = 0; kk < NK; ++kk) {
+                Op8 ka, kb;
+                ka.u = *(const uint4 *)(KA + (kk * 64 + lane) * 8);
+                kb.u = *(const uint4 *)(KB + (kk * 64 + lane) * 8);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    sA[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka.v, qop[t][kk].v, sA[t], 0, 0, 0);
+                    sB[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb.v, qop[t][kk].v, sB[t], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {   // requested here, used behind the softmax
+                vo[dt].h[0] = *(const uint2 *)(VA + (dt * 64 + lane) * 4);
+                vo[dt].h[1] = *(const uint2 *)(VB + (dt * 64 + lane) * 4);
+            }
         }
         const bool whole = is_whole(pp, have);
         uint32_t seen[QT];   // bits 0..15: slots of tile A that the query sees, 16..31: of tile B
@@ -386,50 +422,88 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
             }
         }
         Op8 pop[QT];
+        f32x4 pA[QT], pB[QT];   // the weights of the slots 4 lg + v of each tile
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            float p[8];
 #pragma unroll
-            for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(x[t][v]);
-            l_run[t] += (p[0] + p[1]) + (p[2] + p[3]) + (p[4] + p[5]) + (p[6] + p[7]);
-            pop[t].w[0] = pack_bf16(p[0], p[1]); pop[t].w[1] = pack_bf16(p[2], p[3]);
-            pop[t].w[2] = pack_bf16(p[4], p[5]); pop[t].w[3] = pack_bf16(p[6], p[7]);
+            for (int v = 0; v < 4; ++v) {
+                pA[t][v] = __builtin_amdgcn_exp2f(x[t][v]);
+                pB[t][v] = __builtin_amdgcn_exp2f(x[t][4 + v]);
+            }
+            l_run[t] += (pA[t][0] + pA[t][1]) + (pA[t][2] + pA[t][3]) + (pB[t][0] + pB[t][1]) + (pB[t][2] + pB[t][3]);
+            if constexpr (!F32) {
+                pop[t].w[0] = pack_bf16(pA[t][0], pA[t][1]); pop[t].w[1] = pack_bf16(pA[t][2], pA[t][3]);
+                pop[t].w[2] = pack_bf16(pB[t][0], pB[t][1]); pop[t].w[3] = pack_bf16(pB[t][2], pB[t][3]);
+            }
         }
         // A slot that a query does not see may hold anything, and 0 times a value that is not finite is not 0.  Such values are added one by one for the queries that see them.
         const bool odd = !whole && (strange[buf][0] | strange[buf][1] | strange[buf][2] | strange[buf][3]);
         if (odd) {
 #pragma unroll 1
             for (int slot = 0; slot < 32; ++slot) {
-                const int k = (slot >> 4) * 2 + ((slot & 3) >> 1), from = (slot >> 2 & 3) * 16 + ln;   // the word and the lane of the query's weight for this slot
-                const bf16_t *Vs = (slot < 16 ? VA : VB) + ((slot >> 2 & 3) * 16 + lg * 4) * 4 + (slot & 3);
+                const int from = (slot >> 2 & 3) * 16 + ln;   // the lane that has the query's weight for this slot
+                const T *Vs = (slot < 16 ? VA : VB) + ((slot >> 2 & 3) * 16 + lg * 4) * 4 + (slot & 3);
                 float w[QT];
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
-                    const uint32_t lo = k & 1 ? pop[t].w[1] : pop[t].w[0], hi = k & 1 ? pop[t].w[3] : pop[t].w[2], mine = k & 2 ? hi : lo;
-                    const uint32_t x = (uint32_t)__shfl((int)mine, from);
-                    w[t] = __uint_as_float(slot & 1 ? x & 0xffff0000u : x << 16);
+                    if constexpr (F32) {
+                        const int k = slot & 3;
+                        const f32x4 mine = slot < 16 ? pA[t] : pB[t];
+                        const float lo = k & 1 ? mine[1] : mine[0], hi = k & 1 ? mine[3] : mine[2];
+                        w[t] = __shfl(k & 2 ? hi : lo, from);
+                    } else {
+                        const int k = (slot >> 4) * 2 + ((slot & 3) >> 1);
+                        const uint32_t lo = k & 1 ? pop[t].w[1] : pop[t].w[0], hi = k & 1 ? pop[t].w[3] : pop[t].w[2], mine = k & 2 ? hi : lo;
+                        const uint32_t y = (uint32_t)__shfl((int)mine, from);
+                        w[t] = __uint_as_float(slot & 1 ? y & 0xffff0000u : y << 16);
+                    }
                 }
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const bf16_t v = Vs[dt * 256 + i * 4];
-                        if (finite16(v)) continue;
+                        const float v = to_f<T>(Vs[dt * 256 + i * 4]);
+                        if (finite32(__float_as_uint(v))) continue;
 #pragma unroll
                         for (int t = 0; t < QT; ++t)
-                            if (seen[t] >> slot & 1) O[t][dt][i] += w[t] * bf16_to_f(v);
+                            if (seen[t] >> slot & 1) O[t][dt][i] += w[t] * v;
                     }
             }
+            if constexpr (!F32) {
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!finite16(vo[dt].w[e >> 1] >> ((e & 1) * 16))) vo[dt].w[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+            }
+        }
+        if constexpr (F32) {
+            // a lane's four values are the slots 4 lg + v of feature dt 16 + ln, its weights those of the same slots: a step for each v
+            auto values = [&](auto clean) {
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) {
+                    f32x4 va = *(const f32x4 *)(VA + (dt * 64 + lane) * 4), vb = *(const f32x4 *)(VB + (dt * 64 + lane) * 4);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        if constexpr (clean) {
+                            if (!finite32(__float_as_uint(va[v]))) va[v] = 0.f;
+                            if (!finite32(__float_as_uint(vb[v]))) vb[v] = 0.f;
+                        }
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) {
+                            O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(va[v], pA[t][v], O[t][dt], 0, 0, 0);
+                            O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[v], pB[t][v], O[t][dt], 0, 0, 0);
+                        }
+                    }
+                }
+            };
+            if (odd) values(std::true_type{}); else values(std::false_type{});
+        } else {
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (!finite16(vo[dt].w[e >> 1] >> ((e & 1) * 16))) vo[dt].w[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                for (int t = 0; t < QT; ++t) O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo[dt].v, pop[t].v, O[t][dt], 0, 0, 0);
         }
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-            for (int t = 0; t < QT; ++t) O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo[dt].v, pop[t].v, O[t][dt], 0, 0, 0);
     };
     u32x4 rA[VEC], rB[VEC];   // two pairs in flight: the next one and the one after it
     int hA = 0, hB, h0, h1 = 0;
@@ -460,12 +534,9 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
             if (qi >= QR) continue;
             if (complete) {
                 const float inv = l == 0.f ? 0.f : 1.0f / l;
-                bf16_t *op = (bf16_t *)a.t.t.out + (size_t)(s.first + qi / G) * a.t.t.out_stride + (hk * G + qi % G) * HD + lg * 4;
+                T *op = (T *)a.t.t.out + (size_t)(s.first + qi / G) * a.t.t.out_stride + (hk * G + qi % G) * HD + lg * 4;
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    const f32x4 o = O[t][dt] * inv;
-                    *(uint2 *)(op + dt * 16) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
-                }
+                for (int dt = 0; dt < ND; ++dt) store4(op + dt * 16, O[t][dt] * inv);
             } else {
                 const size_t at = ((size_t)id * 2 + (part > 0)) * QB + wave * 16 * QT + t * 16 + ln;
                 float *op = a.part_o + at * HD + lg * 4;
@@ -479,7 +550,7 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
 }
 
 // The parts of a block: out = sum_c 2^{m_c - M} o_c / sum_c 2^{m_c - M} l_c.  One workgroup 16 queries, 16 threads a query.
-template <int HD, int QT>
+template <typename T, int HD, int QT>
 __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
 {
     constexpr int QB = 64 * QT, V4 = HD / 4, PER = (V4 + 15) / 16;
@@ -514,16 +585,25 @@ __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
             if (x + 16 * i < V4) o[i] += src[x + 16 * i] * w;
     }
     const float inv = L == 0.f ? 0.f : 1.0f / L;
-    bf16_t *op = (bf16_t *)a.t.t.out + (size_t)(s.first + qi / G) * a.t.t.out_stride + (hk * G + qi % G) * HD;
+    T *op = (T *)a.t.t.out + (size_t)(s.first + qi / G) * a.t.t.out_stride + (hk * G + qi % G) * HD;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if (x + 16 * i < V4) *(uint2 *)(op + (x + 16 * i) * 4) = make_uint2(pack_bf16(o[i][0] * inv, o[i][1] * inv), pack_bf16(o[i][2] * inv, o[i][3] * inv));
+        if (x + 16 * i < V4) store4(op + (x + 16 * i) * 4, o[i] * inv);
 }
 
 // Queries of a wavefront in units of 16: by the most queries that a kv head has in a sequence.  One for up to 64, so that all four wavefronts have some; beyond, two, which reads
-// every tile half as often from memory and LDS.  us, one / two: 64 sequences of 3072 positions, 7 queries 84 / 87, 56 queries 100 / 104, up to 112 queries 132 / 110;  4 trees of 1200 to
+// every tile half as often from memory and LDS.  us, one / two: 64 sequences of 3000 positions, 7 queries 84 / 87, 56 queries 100 / 104, up to 112 queries 132 / 110;  4 trees of 1200 to
 // 2048 queries over 6144 positions 116 / 98.  Three would need more registers than two workgroups a unit leave (98 -> 122).
 int query_tiles(int queries) { return queries <= 64 ? 1 : 2; }
+
+// fp32 calls that one launch of tree_rows_k serves faster: by the length of the longest prefix as the caller names it or what the table holds (a wrong one costs time, nothing else), and the
+// keys that all rows read together.  us, rows / matrix cores: 1 sequence of 300 positions, 8 nodes, 4 heads 14.8 / 17.4;  500 positions, 12 nodes, 12 heads 14.6 / 21.0;  3 of 700, 30 nodes,
+// 6 heads 14.4 / 19.7;  beyond: 1 of 4000, 12 nodes, 12 heads 71.7 / 42.9;  4 of 1000, 16 nodes, 28 heads 84.4 / 34.5;  4 of 4000, 128 nodes, 40 heads 8305 / 388 (108 TFLOP/s).
+bool few_rows(const sdlm_kv &kv, const sdlm_tree_args &t)
+{
+    const double len = t.max_len ? t.max_len : (double)kv.pages_per_seq * PAGE;
+    return kv.dtype == 0 && len <= 1024 && (double)t.n_rows * t.n_q_heads * (len + t.max_nodes) <= 512.0 * 1024;
+}
 
 struct Shape { int qt, groups; long blocks; };
 
@@ -531,24 +611,26 @@ Shape shape_of(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
 {
     Shape s;
     const int queries = max_nodes * (n_q_heads / kv.n_kv_heads);
-    s.qt = query_tiles(queries);
+    s.qt = kv.dtype == 0 ? 1 : query_tiles(queries);   // fp32: tiles of twice the bytes
     s.blocks = (long)n_seqs * ((queries + 64 * s.qt - 1) / (64 * s.qt));
     s.groups = kv.n_kv_heads >= SLOTS ? 1 : SLOTS / kv.n_kv_heads;
     return s;
 }
 
-template <int HD, int QT>
+template <typename T, int HD, int QT>
 void mfma_go(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 {
     const unsigned n = (unsigned)(sh.groups * a.t.kv.n_kv_heads + 7) / 8 * 8;
-    hipLaunchKernelGGL((tree_mfma_k<HD, QT>), dim3(n), dim3(256), 0, s, a);
-    hipLaunchKernelGGL((tree_merge_k<HD, QT>), dim3(sh.blocks * 4 * QT, a.t.kv.n_kv_heads), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((tree_mfma_k<T, HD, QT>), dim3(n), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((tree_merge_k<T, HD, QT>), dim3(sh.blocks * 4 * QT, a.t.kv.n_kv_heads), dim3(256), 0, s, a);
 }
 
 template <int HD>
 void mfma_t(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 {
-    if (sh.qt == 1) mfma_go<HD, 1>(s, a, sh); else mfma_go<HD, 2>(s, a, sh);
+    if (a.t.kv.dtype == 0) mfma_go<float, HD, 1>(s, a, sh);
+    else if (sh.qt == 1) mfma_go<bf16_t, HD, 1>(s, a, sh);
+    else mfma_go<bf16_t, HD, 2>(s, a, sh);
 }
 
 void rows(hipStream_t s, const TreeArgs &a)
@@ -572,7 +654,6 @@ bool tree_fits(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
 
 size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes, int max_len)
 {
-    if (kv.dtype == 0) return 256;
     const Shape sh = shape_of(kv, n_q_heads, n_seqs, max_nodes);
     return (size_t)sh.groups * kv.n_kv_heads * 2 * 64 * sh.qt * (kv.head_dim * 4 + 8) + 256;
 }
@@ -583,7 +664,7 @@ void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sd
     a.kv = kv; a.t = t;
     a.pool = (const char *)kv.pool + (size_t)layer * kv.layer_stride * (kv.dtype == 0 ? 4 : 2);
     a.scale = 1.0f / sqrtf((float)kv.head_dim);
-    if (kv.dtype == 0) { rows(s, a); return; }
+    if (few_rows(kv, t)) { rows(s, a); return; }
     MfmaArgs m;
     m.t = a;
     m.G = t.n_q_heads / kv.n_kv_heads;

@@ -1,4 +1,5 @@
 """The operators on the caller's tensors against plain 64-bit implementations of their definitions."""
+import functools
 import math
 
 import numpy as np
@@ -262,6 +263,24 @@ def test_tree_attention_sizes(heads, lens, nodes, dtype, inplace):
     out = run_tree(c)
     check_tree(c, out)
     assert torch.equal(out, run_tree(c, max_len=max(1, max(lens))))      # the hint steers the launch only
+
+
+@pytest.mark.parametrize("heads", HEADS)
+def test_tree_attention_fp32_matrix_cores(heads, monkeypatch):
+    """Small fp32 trees that are named as long ones take the launch of long ones: the same heads, masks and values that are not finite."""
+    monkeypatch.setitem(globals(), "run_tree", functools.partial(run_tree, max_len=4096))
+    test_tree_attention_heads(heads, "fp32")
+    for kind in ("tree", "full", "self", "empty", "random"):
+        c = tree_case(2, heads, [21, 0, 0, 64, 15], [20, 7, 70, 16, 3], "fp32", inplace=kind == "random", kind=kind)
+        check_tree(c, run_tree(c))
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_tree_attention_fp32_matrix_cores_non_finite(value, monkeypatch):
+    monkeypatch.setitem(globals(), "run_tree", functools.partial(run_tree, max_len=4096))
+    test_tree_attention_non_finite_nodes(value, "fp32")
+    for inplace in (False, True):
+        test_tree_attention_ignores_what_is_not_seen(inplace, "fp32")
 
 
 def test_tree_attention_of_one_node_is_a_single_token():
