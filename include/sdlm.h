@@ -362,7 +362,7 @@ typedef struct {
     const void *logits;        /* [dev] rows x vocab, element type `dtype` */
     int64_t row_stride;        /* elements between rows, >= vocab */
     int32_t dtype;             /* 0: fp32, 1: bf16 */
-    int32_t rows, vocab;       /* rows >= 0; vocab 1 .. 524288 */
+    int32_t rows, vocab;       /* rows 0 .. 1048576, rows * ((vocab + 7) / 16384 + 1) at most 2^24; vocab 1 .. 524288 */
     const float *temperature;  /* [dev, rows] or NULL: 1 */
     const int32_t *top_k;      /* [dev, rows] or NULL: off */
     const float *top_p, *min_p;/* [dev, rows] or NULL: off */
@@ -385,10 +385,10 @@ typedef struct {
     void *pool;                /* 16-byte aligned */
     int64_t layer_stride;      /* elements between layers, a multiple of 8 (fp32: 4) */
     int32_t n_layers, n_tiles; /* n_tiles: tiles in a layer */
-    int32_t n_kv_heads, head_dim;   /* head_dim 32, 64, 96 or 128 */
+    int32_t n_kv_heads, head_dim;   /* head_dim 32, 64, 96 or 128; n_kv_heads up to 65535, with the layers 2^23 */
     int32_t dtype;             /* 0: fp32, 1: bf16 */
     int32_t n_pages;
-    int32_t max_seqs, pages_per_seq;
+    int32_t max_seqs, pages_per_seq;   /* up to 2^20, 2^26 */
     int32_t *page_table;       /* max_seqs x pages_per_seq; -1: no page */
     int32_t *lengths;          /* max_seqs: positions that hold K/V */
     int32_t *backed;           /* max_seqs: pages that the sequence holds */
@@ -431,7 +431,7 @@ int sdlm_tree_attention(const sdlm_kv *kv, int32_t layer, const sdlm_tree_args *
  * Make n_new sequences out of the cache's present ones: sequence b becomes what sequence parent[b] is now (-1: an empty one), and sequences from n_new on become empty.  A parent may be
  * named many times (samples of one prompt, a beam's survivors) or not at all, which frees it.
  *   share != 0: the first lengths / 16 pages, which are full, are held in common; the others (the one that is being written, and pages backed ahead) are each sequence's own.
- *   share == 0: all pages are.
+ *   share == 0: all pages are.  (Pages that sequences hold in common since an earlier call stay with those that keep them.)
  * Own pages stay with a sequence that is its own parent, or else with the first that has it as its parent; the others take free pages, the lowest first, in the
  * order of sequences and positions, with the contents copied where a page has positions below lengths.  Pages that nobody holds any more are free at once, for this call too.
  * A sequence must not write to positions below the length that it was forked with, and its length must not fall below that while it shares pages.
@@ -443,7 +443,7 @@ int sdlm_kv_fork(const sdlm_kv *kv, const int32_t *parent, int32_t n_new, int32_
 
 /*
  * Move the K/V of accepted tree nodes into the cache, in every layer: node path[b * path_stride + i] of sequence b to position lengths[b] + i, for i < path_len[b] (at most max_path).
- * Nodes are found as in sdlm_tree_attention.  A path has to ascend.  The destination's pages must be in the table, and not shared.  Nodes or positions without a page
+ * Nodes are found as in sdlm_tree_attention.  A path has to ascend, without repetitions.  The destination's pages must be in the table, and not shared.  Nodes or positions without a page
  * are passed over.  lengths is left as it is: the caller adds path_len when it publishes the tokens, and until then the call may be repeated, unless the nodes stand
  * behind the sequence in its own pages, where it overwrites them.
  */

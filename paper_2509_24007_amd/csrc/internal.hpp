@@ -214,7 +214,7 @@ void launch_fork_state(hipStream_t s, const SeqState &st, const int32_t *parent,
 void launch_sample_accept(hipStream_t s, const SeqState &st, const int32_t *ids, const float *logits, int V, int B, int D, int conf_fn, float tau, int rule, int32_t *ids_out, int32_t *count_out,
                           float *conf_out);
 void launch_assemble_tree(hipStream_t s, const SeqState &st, const RowMeta &rm, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int mask_id,
-                          int staging_base, int causal, int V);
+                          int staging_base, int causal, int V, int max_pos);   // max_pos: entries of the rotation table
 void launch_tree_accept(hipStream_t s, const SeqState &st, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int32_t *path, int32_t *count, int32_t *next);
 void launch_tree_commit(hipStream_t s, const SeqState &st, const TreeState &tr, int B, int D, int paged, int pages_per_seq);
 void launch_read_kv(hipStream_t s, int dtype, const void *pool_layer, const KvGeom &kg, const SeqState &st, int seq,

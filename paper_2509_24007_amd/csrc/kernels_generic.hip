@@ -1265,7 +1265,7 @@ __device__ inline bool tree_node(const int32_t *tokens, const int32_t *parents, 
 // With D = 1 the two are one row.  Only the first block row goes through the LM head.  All K/V are staged: row r of a sequence in slot r of its D staging tiles; a row's mask names the slots
 // that it sees.  One workgroup a sequence.
 __global__ __launch_bounds__(64) void assemble_tree_k(SeqState st, RowMeta rm, TreeState tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int mask_id, int stg0,
-                                                      int causal, int V)
+                                                      int causal, int V, int max_pos)
 {
     const int b = blockIdx.x, per = tree_rows_per_node(D), R = T * per, n = st.n[b], tile0 = stg0 + B + b * D;
     const int32_t *tok = tokens + b * T, *par = parents + b * T;
@@ -1294,7 +1294,7 @@ __global__ __launch_bounds__(64) void assemble_tree_k(SeqState st, RowMeta rm, T
         const int node = i < T ? i : (i - T) / D, j = i < T ? 0 : (i - T) % D, r = b * R + i;   // j: row of the block
         const bool ok = tree_node(tok, par, node, V), block = i >= T;
         rm.tok[r] = j > 0 ? mask_id : ok ? tok[node] : 0;
-        rm.pos[r] = n + depth[node] - 1 + j;
+        rm.pos[r] = min(n + depth[node] - 1 + j, max_pos - 1);   // beyond the last position only where a caller's graph has committed past the host's bounds: such a tree cannot be published
         rm.seq[r] = b; rm.kind[r] = i % PAGE; rm.lim[r] = n;
         rm.stg[r] = tile0 + i / PAGE; rm.smask[r] = 0; rm.stg2[r] = -1;
         if (block ? j == 0 : D < 2) tr.blk_row[b * T + node] = r;
@@ -1306,9 +1306,9 @@ __global__ __launch_bounds__(64) void assemble_tree_k(SeqState st, RowMeta rm, T
 }
 
 void launch_assemble_tree(hipStream_t s, const SeqState &st, const RowMeta &rm, const TreeState &tr, const int32_t *tokens, const int32_t *parents, int B, int D, int T, int mask_id,
-                          int staging_base, int causal, int V)
+                          int staging_base, int causal, int V, int max_pos)
 {
-    hipLaunchKernelGGL(assemble_tree_k, dim3(B), dim3(64), 0, s, st, rm, tr, tokens, parents, B, D, T, mask_id, staging_base, causal, V);
+    hipLaunchKernelGGL(assemble_tree_k, dim3(B), dim3(64), 0, s, st, rm, tr, tokens, parents, B, D, T, mask_id, staging_base, causal, V, max_pos);
 }
 
 // Down the tree from the root: at each point the child whose token is the model's own prediction there (the lowest such node), until there is none.  The root's prediction is the

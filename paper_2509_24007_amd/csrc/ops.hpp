@@ -6,6 +6,8 @@ namespace sdlm {
 
 // ---- drawing tokens from logits (sample.hip)
 constexpr int SAMPLE_MAX_V = 1 << 19;   // weights are 44-bit fixed point: their sum over a row stays inside 64 bits
+constexpr int SAMPLE_MAX_ROWS = 1 << 20;
+bool sample_fits(int rows, int vocab);   // one launch holds them
 size_t sample_workspace_bytes(int rows, int vocab);
 void launch_sample(hipStream_t s, const sdlm_sample_args &a, void *workspace);
 

@@ -26,6 +26,7 @@ int launched(const char *what)
 }
 
 constexpr int MAX_TABLE = 1 << 26;   // entries of a sequence's table: positions fit 31 bits
+constexpr int MAX_SEQS = 1 << 20, MAX_HEADS = 65535, MAX_LAYER_HEADS = 1 << 23;   // grids: workgroups along y, threads along x
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
@@ -45,7 +46,8 @@ int check_kv(const sdlm_kv *kv, bool pages)
     if (kv->head_dim != 32 && kv->head_dim != 64 && kv->head_dim != 96 && kv->head_dim != 128) return bad(SDLM_EINVAL, "head_dim must be 32, 64, 96 or 128");
     if (kv->n_layers < 1 || kv->n_tiles < 1 || kv->n_kv_heads < 1 || kv->max_seqs < 1 || kv->pages_per_seq < 1) return bad(SDLM_EINVAL, "bad cache sizes");
     if (kv->pages_per_seq > MAX_TABLE) return bad(SDLM_EINVAL, "pages_per_seq is at most %d", MAX_TABLE);
-    if ((long)kv->n_layers * kv->n_kv_heads > (1l << 30)) return bad(SDLM_EINVAL, "too many layers and heads");
+    if (kv->n_kv_heads > MAX_HEADS || (long)kv->n_layers * kv->n_kv_heads > MAX_LAYER_HEADS) return bad(SDLM_EINVAL, "too many layers and heads: n_kv_heads is at most %d, n_layers * n_kv_heads %d", MAX_HEADS, MAX_LAYER_HEADS);
+    if (kv->max_seqs > MAX_SEQS) return bad(SDLM_EINVAL, "max_seqs is at most %d", MAX_SEQS);
     if (kv->layer_stride < (int64_t)(kv->n_layers > 1 ? kv->n_tiles : 0) * kv->n_kv_heads * 2 * PAGE * kv->head_dim || kv->layer_stride % (kv->dtype == 0 ? 4 : 8))
         return bad(SDLM_EINVAL, "layer_stride must hold the tiles of a layer and be a multiple of 16 bytes");
     if (!kv->page_table || !kv->lengths) return bad(SDLM_EINVAL, "page_table and lengths are required");
@@ -57,11 +59,11 @@ int check_kv(const sdlm_kv *kv, bool pages)
     return SDLM_OK;
 }
 
-bool sample_sizes(int rows, int vocab) { return rows >= 0 && vocab >= 1 && vocab <= SAMPLE_MAX_V; }
+bool sample_sizes(int rows, int vocab) { return rows >= 0 && vocab >= 1 && vocab <= SAMPLE_MAX_V && sample_fits(rows, vocab); }
 
 bool tree_sizes(int n_q_heads, int n_kv_heads, int n_seqs, int max_nodes, int max_len)
 {
-    return n_q_heads >= 1 && n_q_heads % n_kv_heads == 0 && n_seqs >= 0 && max_nodes >= 1 && max_nodes <= TREE_MAX_NODES && max_len >= 0;
+    return n_q_heads >= 1 && n_q_heads <= MAX_HEADS && n_q_heads % n_kv_heads == 0 && n_seqs >= 0 && max_nodes >= 1 && max_nodes <= TREE_MAX_NODES && max_len >= 0;
 }
 
 }  // namespace
@@ -75,7 +77,7 @@ size_t sdlm_sample_workspace_bytes(int32_t rows, int32_t vocab) { return sample_
 int sdlm_sample(const sdlm_sample_args *a, void *workspace, size_t bytes, void *hip_stream)
 {
     if (!a) return bad(SDLM_EINVAL, "null arguments");
-    if (!sample_sizes(a->rows, a->vocab)) return bad(SDLM_EINVAL, "%d rows of %d logits: rows must be >= 0, vocab 1 .. %d", a->rows, a->vocab, SAMPLE_MAX_V);
+    if (!sample_sizes(a->rows, a->vocab)) return bad(SDLM_EINVAL, "%d rows of %d logits: rows must be 0 .. %d, vocab 1 .. %d, and a launch hold them", a->rows, a->vocab, SAMPLE_MAX_ROWS, SAMPLE_MAX_V);
     if (a->dtype != 0 && a->dtype != 1) return bad(SDLM_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
     if (a->row_stride < a->vocab) return bad(SDLM_EINVAL, "row_stride is less than vocab");
     if (a->rows == 0) return SDLM_OK;
@@ -91,7 +93,7 @@ size_t sdlm_tree_attention_workspace_bytes(const sdlm_kv *kv, int32_t n_q_heads,
 {
     if (check_kv(kv, false)) return 0;
     if (!tree_sizes(n_q_heads, kv->n_kv_heads, n_seqs, max_nodes, max_len)) {
-        bad(SDLM_EINVAL, "n_q_heads must be a multiple of n_kv_heads, max_nodes 1 .. %d, n_seqs and max_len not negative", TREE_MAX_NODES);
+        bad(SDLM_EINVAL, "n_q_heads must be a multiple of n_kv_heads up to %d, max_nodes 1 .. %d, n_seqs and max_len not negative", MAX_HEADS, TREE_MAX_NODES);
         return 0;
     }
     if (!tree_fits(*kv, n_q_heads, n_seqs, max_nodes)) {
@@ -108,7 +110,7 @@ int sdlm_tree_attention(const sdlm_kv *kv, int32_t layer, const sdlm_tree_args *
     if (!t) return bad(SDLM_EINVAL, "null arguments");
     if (layer < 0 || layer >= kv->n_layers) return bad(SDLM_EINVAL, "layer %d outside 0..%d", layer, kv->n_layers - 1);
     if (!tree_sizes(t->n_q_heads, kv->n_kv_heads, t->n_seqs, t->max_nodes, t->max_len))
-        return bad(SDLM_EINVAL, "n_q_heads must be a multiple of n_kv_heads, max_nodes 1 .. %d, n_seqs and max_len not negative", TREE_MAX_NODES);
+        return bad(SDLM_EINVAL, "n_q_heads must be a multiple of n_kv_heads up to %d, max_nodes 1 .. %d, n_seqs and max_len not negative", MAX_HEADS, TREE_MAX_NODES);
     if (t->n_seqs > kv->max_seqs) return bad(SDLM_EINVAL, "%d sequences, the cache has %d", t->n_seqs, kv->max_seqs);
     if (t->n_rows < 0 || (long)t->n_rows > (long)t->n_seqs * t->max_nodes) return bad(SDLM_EINVAL, "%d rows for %d sequences of at most %d nodes", t->n_rows, t->n_seqs, t->max_nodes);
     if (t->mask_words < (t->max_nodes + 63) / 64) return bad(SDLM_EINVAL, "mask_words is too small for max_nodes");

@@ -47,7 +47,7 @@ struct Weigh {
     {
         if ((double)z == M) return (u64)ONE;   // also where the largest is infinite
         const double y = ((double)z - M) * c;
-        return y < -46.0 ? 0ull : (u64)(exp2(y) * ONE + 0.5);
+        return y >= -46.0 ? (u64)(exp2(y) * ONE + 0.5) : 0ull;   // nothing either where both are infinite, the largest logit and the temperature
     }
 };
 
@@ -638,7 +638,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
         double total = 0.0;
         if (by_min) {
             const double z = (double)M + (double)t * log(fmin((double)mp, 1.0));
-            lo = M == INFINITY ? kmax : key_of((float)(z - (fabs(z) + fabs((double)M)) * 1e-6 - 1e-30));   // a little below: the weights decide
+            lo = M == INFINITY ? kmax : t == INFINITY ? 0 : key_of((float)(z - (fabs(z) + fabs((double)M)) * 1e-6 - 1e-30));   // a little below: the weights decide
             if (p < 1.f) {       // top_p is a share of the whole row
                 const double top = (double)M * cs;
                 done = fabs(top) < Y_MAX - 64.0;
@@ -729,7 +729,9 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             const u64 before = block_scan(sh, m, &all);
             block_scan(sh, rest, &rest_all);
             const u64 total = all + rest_all;
-            // The bin in which the running weight passes `bound`, and the token of it that does.
+            // The bin in which the running weight passes `bound`, and the token of it that does.  The bins' sums are rounded otherwise than the tokens' own, so that a bound just below
+            // the weight that top_p keeps may seem to lie behind the cut's bin: it is the cut's token then, which *p holds.
+            int cut = BINS;
             auto locate = [&](u64 bound, bool above, Picked *p) -> bool {
                 if (tid == 0) sh.hit = -1;
                 __syncthreads();
@@ -739,7 +741,9 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                 const int b = sh.hit;
                 const u64 base = sh.acc_mass;
                 __syncthreads();
+                if (cut < BINS && (b < 0 || b > cut)) return true;
                 if (b < 0) return false;   // among the lightest
+                if (!above) cut = b;
                 const int bin = b - PER_OCTAVE * ref;
                 // logits of the bin, a little widened: -bin / PER_OCTAVE >= y > -(bin + 1) / PER_OCTAVE
                 const double zh = -(double)bin / PER_OCTAVE / cs, zl = -(double)(bin + 1) / PER_OCTAVE / cs, wide = (fabs(zh) + fabs(zl)) * 1e-6 + 1e-30;
@@ -802,6 +806,8 @@ void sample_t(hipStream_t s, const sdlm_sample_args &a, const SampleWs &ws)
 }
 
 }  // namespace
+
+bool sample_fits(int rows, int vocab) { return rows <= SAMPLE_MAX_ROWS && (double)rows * n_chunks(vocab, 2) < (double)(1 << 24); }   // threads of a launch fit 32 bits
 
 size_t sample_workspace_bytes(int rows, int vocab)
 {

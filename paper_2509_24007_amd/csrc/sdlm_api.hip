@@ -982,7 +982,7 @@ int sdlm_verify_tree(sdlm_ctx *c, int32_t n_nodes, const int32_t *tokens, const 
         if (tight()) return fail(c, SDLM_ECAPACITY, "%d nodes and a block of %d behind the longest sequence exceed max_seq_len %d", T, D, c->r.max_seq_len);
     }
     hipStream_t s = c->stream;
-    { Phase p(c, SDLM_PH_ROWS); launch_assemble_tree(s, c->st, c->rm, c->tr, tokens, parents, B, D, T, c->m.mask_token_id, c->kg.staging_base, c->m.block_causal, c->m.vocab); }
+    { Phase p(c, SDLM_PH_ROWS); launch_assemble_tree(s, c->st, c->rm, c->tr, tokens, parents, B, D, T, c->m.mask_token_id, c->kg.staging_base, c->m.block_causal, c->m.vocab, c->r.max_seq_len + 2 * D); }
     sdlm_tree_args t = {};
     t.q = c->q; t.out = c->att; t.q_stride = t.out_stride = (int64_t)c->m.n_q_heads * c->m.head_dim;
     t.n_rows = rows; t.n_seqs = B; t.n_q_heads = c->m.n_q_heads; t.max_nodes = R; t.max_len = longest_of_step(c);

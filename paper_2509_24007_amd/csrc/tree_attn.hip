@@ -649,7 +649,7 @@ void rows(hipStream_t s, const TreeArgs &a)
 bool tree_fits(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
 {
     const long pairs = (kv.pages_per_seq + (max_nodes + 2 * PAGE - 2) / PAGE + 1) / 2, blocks = ((long)max_nodes * (n_q_heads / kv.n_kv_heads) + 63) / 64;
-    return (double)n_seqs * blocks * pairs < 2147000000.0;
+    return (double)n_seqs * blocks * pairs < 2147000000.0 && (double)n_seqs * blocks < (double)(1 << 21);   // the second launch: 4 or 8 workgroups of 256 threads a block
 }
 
 size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes, int max_len)

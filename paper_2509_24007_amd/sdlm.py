@@ -361,6 +361,8 @@ class Context:
     def fork(self, parents: Sequence[int]) -> None:
         """The new batch's sequence b continues sequence parents[b]; the others end (sdlm_fork).  Synchronises."""
         p = [int(v) for v in parents]
+        if not all(-2 ** 31 <= v < 2 ** 31 for v in p):
+            _refuse("parents must be 32-bit integers")
         self._check(self.L.sdlm_fork(self.h, len(p), (C.c_int32 * max(1, len(p)))(*p)))
         self.batch = len(p)
 
@@ -492,7 +494,7 @@ class KvCache:
 
     def __init__(self, pool: torch.Tensor, *, page_table: torch.Tensor, lengths: torch.Tensor, n_pages: int = 0, backed: Optional[torch.Tensor] = None,
                  page_refs: Optional[torch.Tensor] = None, free_pages: Optional[torch.Tensor] = None, free_count: Optional[torch.Tensor] = None):
-        if not (pool.is_cuda and pool.dim() == 5 and pool.dtype in _DTYPES and pool.shape[3] == 2 and pool.shape[4] % PAGE == 0):
+        if not (pool.is_cuda and pool.dim() == 5 and pool.numel() and pool.dtype in _DTYPES and pool.shape[3] == 2 and pool.shape[4] % PAGE == 0):
             _refuse("pool must be [layers, tiles, kv heads, 2, 16 * head_dim] fp32 or bf16 on a GPU")
         if not (pool[0].is_contiguous()):
             _refuse("a layer of the pool must be contiguous")
@@ -537,7 +539,8 @@ class KvCache:
 def tree_attention(kv: KvCache, layer: int, q: torch.Tensor, node_offsets: torch.Tensor, mask: torch.Tensor, *, node_table: torch.Tensor, max_nodes: int,
                    node_base: Optional[torch.Tensor] = None, max_len: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of drafted token trees over one layer of the cache (see sdlm_tree_attention): q [nodes, query heads, head_dim] of the cache's type, rows node_offsets[b] up to
-    node_offsets[b + 1] belong to sequence b; mask [nodes, words] int64, bit j of a row: the node sees node j of its sequence.  Returns out, shaped as q."""
+    node_offsets[b + 1] belong to sequence b; mask [nodes, words] int64, bit j of a row: the node sees node j of its sequence.  Returns out, shaped as q; rows outside node_offsets
+    are left as they are."""
     L, dev = load(), kv.device
     if not (q.dim() == 3 and q.shape[2] == kv.head_dim and q.dtype == kv.dtype and q.device == dev):
         _refuse("q must be [nodes, query heads, head_dim] of the cache's type and device")

@@ -395,6 +395,89 @@ def test_samples_forks_and_trees_together():
     ctx.close()
 
 
+def test_captured_samples_and_trees():
+    """A sampled step with its commit and a verified tree with its own, each in a caller's graph, replayed in turn: an eager context on the same inputs draws, accepts and publishes the same."""
+    D, T, B = 4, 6, 2
+    side = torch.cuda.Stream()
+    eager, om, m, tol, _ = setup("fp32", [33, 18], D)
+    replayed = setup("fp32", [33, 18], D, stream=side)[0]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    u = torch.zeros(B, D, device="cuda")
+    tokens, parents = torch.zeros(B, T, **i32), torch.zeros(B, T, **i32)
+    outs = []
+    for _ in range(2):
+        outs.append(dict(ids=torch.zeros(B, D, **i32), count=torch.zeros(B, **i32), z=torch.zeros(B, D, m.vocab, device="cuda"), drawn=torch.zeros(B, D, **i32), n=torch.zeros(B, **i32),
+                         path=torch.zeros(B, T, **i32), g=torch.zeros(B, **i32), next=torch.zeros(B, **i32)))
+    torch.cuda.synchronize()
+
+    def sampled(ctx, o):
+        ctx.decode_step(o["ids"], o["count"], None, o["z"])
+        ctx.sample_step(o["z"], u, o["drawn"], o["n"])
+        ctx.kv_commit()
+
+    def tree(ctx, o):
+        ctx.decode_step(o["ids"], o["count"], None, o["z"])
+        ctx.verify_tree(tokens, parents, o["path"], o["g"], o["next"])
+        ctx.tree_commit()
+
+    graphs = []
+    for f in (sampled, tree):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side, capture_error_mode="thread_local"):
+            f(replayed, outs[1])
+        graphs.append(graph)
+    rng = np.random.default_rng(3)
+    accepted = 0
+    for step in range(6):
+        u.copy_(torch.from_numpy(rng.random((B, D), dtype=np.float32)))
+        f = (sampled, tree)[step % 2]
+        if f is tree:
+            st = Step(eager, m)
+            tk, pr = grow(eager, m, st, B, T, rng)
+            tokens.copy_(torch.from_numpy(tk))
+            parents.copy_(torch.from_numpy(pr))
+        torch.cuda.synchronize()
+        f(eager, outs[0])
+        graphs[step % 2].replay()
+        torch.cuda.synchronize()
+        names = ("ids", "drawn", "n") if f is sampled else ("ids", "path", "g", "next")
+        for name in names:
+            assert torch.equal(outs[0][name], outs[1][name]), (step, name)
+        accepted += int(outs[0]["g"].sum()) if f is tree else 0
+        assert eager.get_lengths()[0].tolist() == replayed.get_lengths()[0].tolist()
+    assert accepted > 0
+    eager.close()
+    replayed.close()
+
+
+def test_tree_behind_a_callers_graph_that_fills_the_context():
+    """A caller's graph commits until no position is left, which the host does not see: a tree behind it is computed (its positions end with the rotation's) and cannot be published."""
+    D = 4
+    side = torch.cuda.Stream()
+    ctx, om, m, tol, hist = setup("fp32", [20], D, max_batch=1, max_seq_len=64, stream=side)
+    ovr, full = torch.ones(1, D, dtype=torch.int32, device="cuda"), torch.full((1,), D, dtype=torch.int32, device="cuda")
+    ids, cnt = torch.zeros_like(ovr), torch.zeros_like(full)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="thread_local"):
+        ctx.decode_step(ids, cnt)
+        ctx.kv_commit(ovr, full)
+    for _ in range(11):
+        graph.replay()
+    torch.cuda.synchronize()
+    z = torch.zeros(1, 12, m.vocab, device="cuda")
+    chain = torch.arange(-1, 11, dtype=torch.int32, device="cuda")[None].contiguous()
+    ctx.decode_step(ids, cnt)
+    ctx.verify_tree(torch.ones(1, 12, dtype=torch.int32, device="cuda"), chain, logits=z)
+    ctx.tree_commit()
+    torch.cuda.synchronize()
+    assert torch.isfinite(z).all()
+    with pytest.raises(sdlm.SdlmError) as e:
+        ctx.get_lengths()
+    assert e.value.code == sdlm.ECAPACITY
+    ctx.close()
+
+
 def test_described_cache_serves_the_operators():
     """Attention over a context's own cache through sdlm_kv_describe: a node that sees only the cache is a query over it."""
     import ctypes as C

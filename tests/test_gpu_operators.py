@@ -97,6 +97,27 @@ def test_sample_masks_and_non_finite():
             check_sample(z, t, k, p, m, rng.random(10))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_sample_infinite_temperature(dtype):
+    """exp(0) = 1 for every token above -infinity; where the largest logit is infinite too, only the tokens with it have weight."""
+    z, rng = draw_logits(23, 6, 5003, dtype)
+    z[:, ::3] = -math.inf
+    for k, p, m in [(0, 1.0, 0.0), (0, 0.7, 0.0), (0, 1.0, 0.5), (0, 1.0, 1.0), (0, 0.4, 1.0), (50, 0.6, 1.0), (3000, 1.0, 0.0)]:
+        check_sample(z, math.inf, k, p, m, rng.random(6))
+    z[:, 70] = math.inf
+    z[:, 40] = math.inf
+    for kw in (dict(), dict(top_k=dev(np.full(6, 9))), dict(min_p=dev(np.full(6, 0.5), torch.float32)), dict(top_p=dev(np.full(6, 0.9), torch.float32))):
+        ids, prob = sdlm.sample(z, dev([0.0, 0.2, 0.49, 0.5, 0.7, 0.9], torch.float32), temperature=dev(np.full(6, math.inf), torch.float32), **kw)
+        assert ids.cpu().tolist() == [40, 40, 40, 70, 70, 70] and (prob == 0.5).all()
+
+
+@pytest.mark.parametrize("V", [3001, 50021])
+def test_sample_of_the_last_kept_token(V):
+    """u = 1 is the last token that top_p keeps, whatever the bins' rounded sums are: 64 cuts of a row."""
+    z = draw_logits(V, 1, V, "fp32", spread=1.1)[0].repeat(64, 1).contiguous()
+    check_sample(z, 1.0, 0, np.linspace(0.3, 0.999, 64), 0.0, 1.0)
+
+
 def test_sample_uniform_out_of_range_and_defaults():
     z, _ = draw_logits(2, 4, 999, "fp32")
     check_sample(z, 1.0, 0, 1.0, 0.0, [-1.0, 1.0, 7.0, 0.25])

@@ -106,6 +106,24 @@ def test_tree_attention_layer_and_workspace():
     assert L.sdlm_tree_attention(C.byref(kv()), 0, C.byref(tree(n_rows=0)), None, 0, None) == 0
 
 
+BIG = 1 << 50      # a layer stride that holds anything
+
+
+def test_sizes_beyond_a_launch_are_refused():
+    """Grids and their threads have 16 and 32 bits: what does not fit is refused before the first launch."""
+    L = sdlm.load()
+    for rows, vocab in ((1 << 21, 10), ((1 << 20) + 1, 10), (1 << 20, 1 << 19)):
+        assert L.sdlm_sample_workspace_bytes(rows, vocab) == 0
+        refused(L.sdlm_sample(C.byref(sample_args(rows=rows, vocab=vocab, row_stride=vocab)), P, 1 << 62, None), sdlm.EINVAL, "rows")
+    assert L.sdlm_sample_workspace_bytes(1 << 20, 10) > 0
+    for kw, word in ((dict(n_kv_heads=65536, layer_stride=BIG), "heads"), (dict(n_layers=1 << 10, n_kv_heads=1 << 14, layer_stride=BIG), "layers"), (dict(max_seqs=(1 << 20) + 1), "max_seqs")):
+        refused(L.sdlm_kv_fork(C.byref(kv(**kw)), P, 2, 1, P, P, 1 << 62, None), sdlm.EINVAL, word)
+        refused(L.sdlm_kv_compact(C.byref(kv(**kw)), 2, P, 4, P, 4, P, 1, None, None), sdlm.EINVAL, word)
+        refused(L.sdlm_tree_attention(C.byref(kv(**kw)), 0, C.byref(tree()), P, 1 << 62, None), sdlm.EINVAL, word)
+    refused(L.sdlm_tree_attention(C.byref(kv()), 0, C.byref(tree(n_q_heads=65536, q_stride=BIG, out_stride=BIG)), P, 1 << 62, None), sdlm.EINVAL, "n_q_heads")
+    assert L.sdlm_tree_attention_workspace_bytes(C.byref(kv(max_seqs=1 << 20, pages_per_seq=1)), 4, 1 << 20, 1024, 0) == 0
+
+
 def test_struct_sizes_agree_with_the_header():
     """Sizes of the argument structs as a C compiler lays them out on this ABI."""
     assert C.sizeof(sdlm.SampleArgs) == 88 and C.sizeof(sdlm.KvDesc) == 96 and C.sizeof(sdlm.TreeArgs) == 96
