@@ -21,7 +21,7 @@ constexpr int TH = 1024;
 typedef unsigned long long u64;
 constexpr double ONE = 17592186044416.0;   // 2^44
 constexpr double LOG2E = 1.4426950408889634;
-constexpr uint32_t KEY_NEG_INF = 0x007fffffu;
+constexpr uint32_t KEY_NEG_INF = 0x007fffffu, KEY_INF = 0xff800000u;
 
 __device__ inline float canon(float z)   // NaN is never drawn; the two zeros are equal
 {
@@ -247,14 +247,20 @@ struct Pieces {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    static __device__ void values(const uint4 &u, float (&x)[E])
+    static __device__ void bare(const uint4 &u, float (&x)[E])
     {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            if constexpr (sizeof(T) == 4) x[e] = canon(__uint_as_float(w[e]));
-            else x[e] = canon(__uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16));
+            if constexpr (sizeof(T) == 4) x[e] = __uint_as_float(w[e]);
+            else x[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
         }
+    }
+    static __device__ void values(const uint4 &u, float (&x)[E])
+    {
+        bare(u, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = canon(x[e]);
     }
 };
 
@@ -418,9 +424,22 @@ __device__ uint32_t kth_run(Shared &sh, const uint32_t (&keys)[RUNS], int k)
     return prefix << 10;
 }
 
-// Candidates: the logits whose key is at least `lo` and at most `hi` (and, bin >= 0, that fall into this absolute bin), from the runs whose maximum is at least lo.  Returns whether they fit.
+// The smallest key in [k0, k1] whose logit lies in bin `bin` (absolute) or in a heavier one; k1 + 1 if there is none.  By a wavefront: bins do not rise with the logit.
+__device__ uint32_t first_of_bin(uint32_t k0, uint32_t k1, int bin, double cs)
+{
+    uint32_t n = k1 - k0 + 1;
+    while (n > 1) {
+        const uint32_t step = (n + 63) / 64, at = step * ((threadIdx.x & 63) + 1) - 1;
+        const int first = __ffsll(__ballot(at >= n - 1 || bin_of((double)of_key(k0 + at) * cs) <= bin)) - 1;
+        k0 += step * first;
+        n = min(step, n - step * first);
+    }
+    return bin_of((double)of_key(k0) * cs) <= bin ? k0 : k0 + 1;
+}
+
+// Candidates: the logits whose key is at least `lo` and at most `hi`, from the runs whose maximum is at least lo.  Returns whether they fit.
 template <typename T>
-__device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[RUNS], int per, uint32_t lo, uint32_t hi, bool check_bin, int bin, double cs)
+__device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[RUNS], int per, uint32_t lo, uint32_t hi)
 {
     constexpr int E = Pieces<T>::E, N = PER_THREAD / E;
     const int lp = 31 - __clz(per), lg = 31 - __clz(N) - lp;   // log2 of the runs of a thread of the first launch, and of a run's pieces
@@ -431,17 +450,51 @@ __device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[R
         if (keys[j] >= lo && keys[j] > KEY_NEG_INF) ls.run[atomicAdd(&ls.n_run, 1)] = (uint16_t)(threadIdx.x + j * TH);
     __syncthreads();
     const int pieces = ls.n_run << lg;
-    for (int q = threadIdx.x; q < pieces; q += TH) {
-        const int run = ls.run[q >> lg], v = (((run >> 8) << lg) + (q & ((1 << lg) - 1))) * 256 + (run & 255);
-        float x[E];
-        row.values(row.raw(v), x);
+    // The logits that a bound lets in are few of those that are read: two comparisons each, and the rest of the work for those that pass.  A wavefront takes room for all of its trip's
+    // candidates at once: an atomic, and places by counting the lanes in front.
+    constexpr int AT = 8 / E;   // pieces of a trip (us of a batch of 256 x 152064 with top-p .99, temperature 1.3: one 179, two 174, four 202)
+    const float least = of_key(max(lo, KEY_NEG_INF + 1)), most = of_key(min(hi, KEY_INF));
+    for (int q0 = threadIdx.x; q0 < (pieces + 63) / 64 * 64; q0 += AT * TH) {
+        uint4 raw[AT];
+        int i0[AT];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const uint32_t key = key_of(x[e]);
-            if (key < lo || key > hi || key <= KEY_NEG_INF) continue;
-            if (check_bin && bin_of((double)x[e] * cs) != bin) continue;
-            const int at = atomicAdd(&ls.n_cand, 1);
-            if (at < CAND) ls.cand[at] = (u64)key << 32 | (uint32_t)~(uint32_t)(v * E - row.lead + e);
+        for (int k = 0; k < AT; ++k) {
+            const int q = q0 + k * TH;
+            raw[k] = make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);   // not numbers: in no bound
+            i0[k] = 0;
+            if (q < pieces) {
+                const int run = ls.run[q >> lg], v = (((run >> 8) << lg) + (q & ((1 << lg) - 1))) * 256 + (run & 255);
+                raw[k] = row.raw(v);
+                i0[k] = v * E - row.lead;
+            }
+        }
+        u64 who[AT * E];
+        int total = 0;
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            float x[E];
+            row.bare(raw[k], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                who[k * E + e] = __ballot(x[e] >= least && x[e] <= most);
+                total += __popcll(who[k * E + e]);
+            }
+        }
+        if (total == 0) continue;
+        int at = 0;
+        if ((threadIdx.x & 63) == 0) at = atomicAdd(&ls.n_cand, total);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            float x[E];
+            row.bare(raw[k], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const u64 w = who[k * E + e];
+                const int place = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(w >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)w, 0));
+                if ((w >> (threadIdx.x & 63) & 1) && place < CAND) ls.cand[place] = (u64)key_of(canon(x[e])) << 32 | (uint32_t)~(uint32_t)(i0[k] + e);
+                at += __popcll(w);
+            }
         }
     }
     __syncthreads();
@@ -624,7 +677,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
     if (M == -INFINITY) {
         // every token is masked
     } else if (!(t > 0.f)) {
-        if ((done = gather(ls, row, keys, per, kmax, kmax, false, 0, 0.0))) {
+        if ((done = gather(ls, row, keys, per, kmax, kmax))) {
             u64 best = 0;
             for (int i = tid; i < ls.n_cand; i += TH) best = max(best, ls.cand[i]);
             id = (int)~(uint32_t)block_reduce(sh, best, [](u64 x, u64 y) { return x > y ? x : y; });
@@ -657,7 +710,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             done = k <= TOP_MAX;
             lo = done ? kth_run(sh, keys, k) : 0;
         }
-        done = done && gather(ls, row, keys, per, lo, 0xffffffffu, false, 0, 0.0);
+        done = done && gather(ls, row, keys, per, lo, KEY_INF);
         if (done) {
             int n = ls.n_cand;
             const double least = fmin((double)mp, 1.0) * ONE;
@@ -716,16 +769,14 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             __syncthreads();
             const u64 *hist = ws.hist + (size_t)r * chunks * (BINS + 1);
             if (tid < BINS)
-#pragma unroll 4
+#pragma unroll 5
                 for (int c = 0; c < chunks; ++c) {
                     const int back = (int)sh.cnt[c], b = tid - PER_OCTAVE * back;
-                    m += (b >= 0 && back < 46 ? hist[c * (BINS + 1) + b] : 0) >> back;
+                    const u64 *h = hist + (size_t)c * (BINS + 1);
+                    m += (b >= 0 && back < 46 ? h[b] : 0) >> back;
+                    rest += (tid + PER_OCTAVE * back >= BINS && back < 46 ? h[tid] : 0) >> back;   // moved below the last bin
                 }
-            for (int c = 0; c < chunks; ++c) {   // what falls below the last bin
-                const int back = (int)sh.cnt[c];
-                if (back == 46) continue;
-                for (int o = max(BINS - PER_OCTAVE * back, 0) + tid; o <= BINS; o += TH) rest += hist[c * (BINS + 1) + o] >> back;
-            }
+            if (tid < chunks && sh.cnt[tid] < 46) rest += hist[(size_t)tid * (BINS + 1) + BINS] >> sh.cnt[tid];
             const u64 before = block_scan(sh, m, &all);
             block_scan(sh, rest, &rest_all);
             const u64 total = all + rest_all;
@@ -745,9 +796,17 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                 if (b < 0) return false;   // among the lightest
                 if (!above) cut = b;
                 const int bin = b - PER_OCTAVE * ref;
-                // logits of the bin, a little widened: -bin / PER_OCTAVE >= y > -(bin + 1) / PER_OCTAVE
+                // logits of the bin, -bin / PER_OCTAVE >= y > -(bin + 1) / PER_OCTAVE, first a little widened, then as the first launch told them apart
                 const double zh = -(double)bin / PER_OCTAVE / cs, zl = -(double)(bin + 1) / PER_OCTAVE / cs, wide = (fabs(zh) + fabs(zl)) * 1e-6 + 1e-30;
-                if (!gather(ls, row, keys, per, key_of((float)(zl - wide)), key_of((float)(zh + wide)), true, bin, cs) || ls.n_cand == 0) return false;
+                const uint32_t k0 = max(key_of((float)(zl - wide)), KEY_NEG_INF + 1), k1 = min(key_of((float)(zh + wide)), KEY_INF - 1);
+                if (k0 > k1) return false;
+                if (tid < 128) {
+                    const uint32_t k = first_of_bin(k0, k1, tid < 64 ? bin : bin - 1, cs);
+                    if ((tid & 63) == 0) sh.cnt[tid >> 6] = k;
+                }
+                __syncthreads();
+                const uint32_t lo = sh.cnt[0], hi = sh.cnt[1] - 1;
+                if (!gather(ls, row, keys, per, lo, hi) || ls.n_cand == 0) return false;
                 const int n = ls.n_cand;
                 if (n > SORT_ALL) {
                     Fine<FromRef> bins(sh, ls, w, n, base);

@@ -111,6 +111,15 @@ def test_sample_infinite_temperature(dtype):
         assert ids.cpu().tolist() == [40, 40, 40, 70, 70, 70] and (prob == 0.5).all()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,spread", [(700, 1.0), (20011, 0.4), (50021, 1.1), (152064, 1.1), (152064, 2.2)])
+def test_sample_draws_in_front_of_cuts(V, spread, dtype):
+    """The draw in the cut's own bin, in others, in bins of one token and of thousands: 96 cuts and numbers for the same row."""
+    z, rng = draw_logits(V, 1, V, dtype, spread=spread)
+    u = np.concatenate([rng.random(48), 1.0 - rng.random(48) * 0.02])
+    check_sample(z.repeat(96, 1).contiguous(), 1.2, 0, rng.permutation(np.linspace(0.2, 0.995, 96)), 0.0, u)
+
+
 @pytest.mark.parametrize("V", [3001, 50021])
 def test_sample_of_the_last_kept_token(V):
     """u = 1 is the last token that top_p keeps, whatever the bins' rounded sums are: 64 cuts of a row."""
