@@ -449,52 +449,39 @@ __device__ bool gather(Lists &ls, const Pieces<T> &row, const uint32_t (&keys)[R
     for (int j = 0; j < RUNS; ++j)
         if (keys[j] >= lo && keys[j] > KEY_NEG_INF) ls.run[atomicAdd(&ls.n_run, 1)] = (uint16_t)(threadIdx.x + j * TH);
     __syncthreads();
-    const int pieces = ls.n_run << lg;
-    // The logits that a bound lets in are few of those that are read: two comparisons each, and the rest of the work for those that pass.  A wavefront takes room for all of its trip's
-    // candidates at once: an atomic, and places by counting the lanes in front.
-    constexpr int AT = 8 / E;   // pieces of a trip (us of a batch of 256 x 152064 with top-p .99, temperature 1.3: one 179, two 174, four 202)
+    // Bound by its instructions: a unit has a workgroup for all of a row's logits where the bound is low.  So two pieces of a run are one trip, a logit costs two comparisons and a bit, and the rest
+    // is done for those that pass (few), a thread's one behind the other.  A wavefront takes room for all of its trip's candidates with one atomic.
+    const bool two = lg > 0;
+    const int l2 = two ? lg - 1 : 0, trips = ls.n_run << l2;
     const float least = of_key(max(lo, KEY_NEG_INF + 1)), most = of_key(min(hi, KEY_INF));
-    for (int q0 = threadIdx.x; q0 < (pieces + 63) / 64 * 64; q0 += AT * TH) {
-        uint4 raw[AT];
-        int i0[AT];
+    for (int q = threadIdx.x; q < trips; q += TH) {
+        const int run = ls.run[q >> l2], v = (((run >> 8) << lg) + ((q & ((1 << l2) - 1)) << (lg - l2))) * 256 + (run & 255), i0 = v * E - row.lead;
+        const uint4 raw0 = row.raw(v), raw1 = two ? row.raw(v + 256) : make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);   // not numbers: in no bound
+        float x[E], y[E];
+        row.bare(raw0, x);
+        row.bare(raw1, y);
+        uint32_t hits = 0;
 #pragma unroll
-        for (int k = 0; k < AT; ++k) {
-            const int q = q0 + k * TH;
-            raw[k] = make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);   // not numbers: in no bound
-            i0[k] = 0;
-            if (q < pieces) {
-                const int run = ls.run[q >> lg], v = (((run >> 8) << lg) + (q & ((1 << lg) - 1))) * 256 + (run & 255);
-                raw[k] = row.raw(v);
-                i0[k] = v * E - row.lead;
-            }
+        for (int e = 0; e < E; ++e) {
+            hits |= x[e] >= least && x[e] <= most ? 1u << e : 0u;
+            hits |= y[e] >= least && y[e] <= most ? 1u << (E + e) : 0u;
         }
-        u64 who[AT * E];
-        int total = 0;
+        if (!__any(hits)) continue;
+        const int n = __popc(hits);
+        int before = 0, total = 0;
 #pragma unroll
-        for (int k = 0; k < AT; ++k) {
-            float x[E];
-            row.bare(raw[k], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                who[k * E + e] = __ballot(x[e] >= least && x[e] <= most);
-                total += __popcll(who[k * E + e]);
-            }
+        for (int k = 1; k <= 2 * E; k <<= 1) {
+            const u64 w = __ballot(n & k);
+            before += k * (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(w >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)w, 0));
+            total += k * __popcll(w);
         }
-        if (total == 0) continue;
         int at = 0;
-        if ((threadIdx.x & 63) == 0) at = atomicAdd(&ls.n_cand, total);
-        at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-        for (int k = 0; k < AT; ++k) {
-            float x[E];
-            row.bare(raw[k], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const u64 w = who[k * E + e];
-                const int place = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(w >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)w, 0));
-                if ((w >> (threadIdx.x & 63) & 1) && place < CAND) ls.cand[place] = (u64)key_of(canon(x[e])) << 32 | (uint32_t)~(uint32_t)(i0[k] + e);
-                at += __popcll(w);
-            }
+        const int leader = __ffsll(__ballot(1)) - 1;
+        if ((threadIdx.x & 63) == leader) at = atomicAdd(&ls.n_cand, total);
+        at = __builtin_amdgcn_readfirstlane(at) + before;
+        for (; hits; hits &= hits - 1, ++at) {
+            const int e = __ffs((int)hits) - 1, i = i0 + e + (e >= E ? 255 * E : 0);
+            if (at < CAND) ls.cand[at] = (u64)key_of(canon(to_f<T>(row.z[i]))) << 32 | (uint32_t)~(uint32_t)i;
         }
     }
     __syncthreads();
