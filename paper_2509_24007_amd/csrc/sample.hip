@@ -11,6 +11,10 @@
 //   - otherwise the histogram says in which bin the weight passes top_p, and in which bin the draw falls, and the candidates are that bin.
 // Where the candidates do not fit (thousands of equal logits), where top-k is beyond TOP_MAX, or where the exponents leave the histogram's range, the row is searched by digits
 // of the logits' order-preserving integers instead, without sorting, in a dozen passes.
+//
+// us: one row of 151936 fp32 5 + 13, 256 rows of 152064 with mixed settings 50 + 45, 33 rows of 33003 bf16 13 + 27.  The first launch is bound by the read where no row asks for weights (256 rows 39, 4.0 TB/s),
+// else by the weights' instructions.  The second is a chain of scans and synchronisations in one workgroup, whose longest part, where a bound lies far down a flat tail, is the read of the whole row (about
+// 25 each time, by its instructions).  256 rows with top_k = 5000, by digits: 750.
 #include "ops.hpp"
 
 namespace sdlm {

@@ -123,7 +123,9 @@ __global__ __launch_bounds__(256) void tree_rows_k(TreeArgs a)
 // brings to LDS serves the whole block.  A launch has as many workgroups as the chip holds at once, and the tiles of all blocks, one block behind the other, are
 // dealt out to them in equal runs: no unit waits for another at the end, whatever the lengths are.  A workgroup's run may end inside a block; such a part leaves a
 // maximum, a sum and an unnormalised output, and the parts of a block are merged by a second launch.  At most its first and its last part are incomplete, so a
-// workgroup has two places for them.  fp32 tiles and operands take the instruction of 16 x 16 x 4, whose operands are neighbours in the tiles as they are.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
+// workgroup has two places for them.  fp32 tiles and operands take the instruction of 16 x 16 x 4, whose operands are neighbours in the tiles as they are.
+// us, attention and merge: 64 sequences of 2048 to 4096 positions, up to 16 nodes, 28 / 4 heads 100 + 11 (413 MB, bound by the cache);  4 of up to 8192, up to 256 nodes, 16 / 2 heads 85 + 8 (480 TFLOP/s, bound by
+// the vector instructions between the two products);  one of 512, 12 nodes 8 + 6, a chain of round trips.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
