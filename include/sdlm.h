@@ -356,7 +356,7 @@ const char *sdlm_op_error(void);
  *   - w >= min_p (min_p <= 0 or NaN: all);
  * the first is always kept.  Drawn is the first kept token, in that order, whose running weight exceeds u times the weight of all kept ones.  A temperature <= 0 (or NaN)
  * draws the first.  Where the largest logit is +infinity, only the tokens with it have weight.  A row without any token above -infinity gives id -1 and probability 0.
- * Weights are held to 2^-45 of the largest, in integers: a result does not depend on the launch or on the row's neighbours.  A token whose weight is below that is not drawn.
+ * Weights are held to 2^-45 of the largest, and where the whole row counts (no top_k) to 2^-30 of themselves, in integers, equal ones for equal logits: a result does not depend on the launch or on the row's neighbours.  A token whose weight is below that is not drawn.
  */
 typedef struct {
     const void *logits;        /* [dev] rows x vocab, element type `dtype` */

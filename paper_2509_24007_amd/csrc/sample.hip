@@ -2,7 +2,7 @@
 //
 // The tokens of a row are ordered by logit, equal ones by index.  All filters keep a first part of that order, and the uniform number picks from the kept part
 // in that order.  Weights are integers in units of 2^-44 of the largest (or of the power of two above it): their sums do not depend on the order of the threads, and
-// their error (2^-45 a token) is far below the weight of any token that a draw could fall on.
+// their error (2^-45 of the largest a token, and 2^-30 of itself where the histogram counts) is far below the weight of any token that a draw could fall on.
 //
 // Two launches.  The first reads the logits once, all units together: a thread takes 64 of them and leaves the maxima of its runs, and for a row whose filters need the
 // weight of the whole row (no top-k) a workgroup also leaves a histogram of the weights over 1/32 octaves.  The second has a workgroup a row, which sorts only what matters:
@@ -12,7 +12,7 @@
 // Where the candidates do not fit (thousands of equal logits), where top-k is beyond TOP_MAX, or where the exponents leave the histogram's range, the row is searched by digits
 // of the logits' order-preserving integers instead, without sorting, in a dozen passes.
 //
-// us: one row of 151936 fp32 5 + 13, 256 rows of 152064 with mixed settings 50 + 45, 33 rows of 33003 bf16 13 + 27.  The first launch is bound by the read where no row asks for weights (256 rows 39, 4.0 TB/s),
+// us: one row of 151936 fp32 5 + 13, 256 rows of 152064 with mixed settings 51 + 46, 33 rows of 33003 bf16 13 + 28.  The first launch is bound by the read where no row asks for weights (256 rows 39, 4.0 TB/s),
 // else by the weights' instructions.  The second is a chain of scans and synchronisations in one workgroup, whose longest part, where a bound lies far down a flat tail, is the read of the whole row (about
 // 25 each time, by its instructions).  256 rows with top_k = 5000, by digits: 750.
 #include "ops.hpp"
@@ -62,6 +62,7 @@ struct Shared {
     u64 mass[2048];
     uint32_t cnt[2048];
     u64 red[TH / 64];
+    double table[64];   // 2^(j / 64)
     Found f;
     u64 w;
     uint32_t prefix;
@@ -287,19 +288,26 @@ struct SampleWs {
 };
 constexpr int NONE = -(1 << 30);
 
-// 2^d in units of 2^-44, d <= 0, to about 2^-31 of itself: a table of 2^(j / 64) and a cubic for the rest.  Only for the sums of bins; the candidates' own weights are exact.
+// The exponent of 2 of a logit's weight, rounded by itself: both launches have to find the same one, so it is no part of a fused product and sum.
+__device__ inline double exponent(float z, double cs)
+{
+    double y = (double)z * cs;
+    asm("" : "+v"(y));
+    return y;
+}
+
+// 2^d in units of 2^-44, d <= 0: a table of 2^(j / 64) and a cubic for the rest, to 30 bits, which depend on d's fraction alone.  So equal logits have equal weights whatever power of two they
+// are held against, in both launches, and sums of weights down to 2^-14 of the largest are exact: a bound that falls between equal logits falls between the same ones as in the definition.
 __device__ inline u64 fast_weight(double d, const double *table)
 {
-    if (d < -46.0) return 0;
     const double magic = 6755399441055744.0;   // 1.5 2^52: the sum's low bits are the rounded integer
     const double s = d * 64.0 + magic;
     const int n = __double2loint(s);
     const float r = (float)(d - (s - magic) * (1.0 / 64.0)) * 0.69314718056f;   // |r| <= ln 2 / 128
-    const float q = r * (1.f + r * (0.5f + r * 0.16666667f));
+    const float q = r * fmaf(r, fmaf(r, 0.16666667f, 0.5f), 1.f);
     const double t = table[n & 63];
-    const double w = ldexp(fma(t, (double)q, t), n >> 6);
-    const double m2 = 384.0;                   // 1.5 2^8: an ulp of the sum is 2^-44
-    return (u64)(__double_as_longlong(w + m2) - __double_as_longlong(m2));
+    const uint32_t m = (uint32_t)__double2loint(fma(t, (double)q, t) + 6291456.0);   // + 1.5 2^22: an ulp of the sum is 2^-30
+    return ((((u64)m << 15) >> -(n >> 6)) + 1) >> 1;
 }
 
 __device__ inline int bin_of(double y) { return (int)floor(y * -(double)PER_OCTAVE); }   // absolute: bin - PER_OCTAVE ref counts from the reference
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(256) void sample_scan_k(sdlm_sample_args a, SampleW
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const double y = (double)x[i][e] * cs, d = y - ref;
+            const double y = exponent(x[i][e], cs), d = y - ref;
             if (!(d > -46.0)) continue;
             const u64 w = fast_weight(d, table);
             const int b = sum ? BINS : bin_of(y) + PER_OCTAVE * ref;
@@ -434,11 +442,11 @@ __device__ uint32_t first_of_bin(uint32_t k0, uint32_t k1, int bin, double cs)
     uint32_t n = k1 - k0 + 1;
     while (n > 1) {
         const uint32_t step = (n + 63) / 64, at = step * ((threadIdx.x & 63) + 1) - 1;
-        const int first = __ffsll(__ballot(at >= n - 1 || bin_of((double)of_key(k0 + at) * cs) <= bin)) - 1;
+        const int first = __ffsll(__ballot(at >= n - 1 || bin_of(exponent(of_key(k0 + at), cs)) <= bin)) - 1;
         k0 += step * first;
         n = min(step, n - step * first);
     }
-    return bin_of((double)of_key(k0) * cs) <= bin ? k0 : k0 + 1;
+    return bin_of(exponent(of_key(k0), cs)) <= bin ? k0 : k0 + 1;
 }
 
 // Candidates: the logits whose key is at least `lo` and at most `hi`, from the runs whose maximum is at least lo.  Returns whether they fit.
@@ -523,26 +531,6 @@ __device__ void sort(u64 *v, int n)
         }
 }
 
-// Running weights of the first n candidates (w: of a logit), starting at `base`.
-template <typename W>
-__device__ void weigh(Shared &sh, Lists &ls, int n, u64 base, const W &w)
-{
-    u64 v[CAND / TH], s = 0, all;
-    const int i0 = threadIdx.x * (CAND / TH);
-#pragma unroll
-    for (int j = 0; j < CAND / TH; ++j) {
-        v[j] = i0 + j < n ? w(of_key((uint32_t)(ls.cand[i0 + j] >> 32))) : 0;
-        s += v[j];
-    }
-    u64 at = base + block_scan(sh, s, &all);
-#pragma unroll
-    for (int j = 0; j < CAND / TH; ++j) {
-        at += v[j];
-        if (i0 + j < n) ls.cum[i0 + j] = at;
-    }
-    __syncthreads();
-}
-
 // The first of n candidates whose running weight is at least (above) `bound`; n if there is none.
 __device__ int first_past(const Lists &ls, int n, u64 bound, bool above)
 {
@@ -557,30 +545,45 @@ __device__ int first_past(const Lists &ls, int n, u64 bound, bool above)
 __device__ inline int index_at(const Lists &ls, int i) { return (int)~(uint32_t)ls.cand[i]; }
 __device__ inline float logit_at(const Lists &ls, int i) { return of_key((uint32_t)(ls.cand[i] >> 32)); }
 
-struct FromRef {   // weight against a power of two
+struct Weight {   // against a power of two, as the first launch has it, or against the largest (table: null); one type, so that what takes weights is there once
     double cs, ref;
+    const double *table;
     __device__ u64 operator()(float z) const
     {
-        const double d = (double)z * cs - ref;
-        return d < -46.0 ? 0ull : (u64)(exp2(d) * ONE + 0.5);
+        if (!table) return Weigh{ref, cs}(z);
+        const double d = exponent(z, cs) - ref;
+        return d > -46.0 ? fast_weight(d, table) : 0ull;
     }
 };
+
+// Running weights of the first n candidates, starting at `base`.
+__device__ void weigh(Shared &sh, Lists &ls, int n, u64 base, const Weight &w)
+{
+    for (int i0 = 0; i0 < n; i0 += TH) {
+        const int i = i0 + threadIdx.x;
+        const u64 x = i < n ? w(of_key((uint32_t)(ls.cand[i] >> 32))) : 0;
+        u64 all;
+        const u64 before = base + block_scan(sh, x, &all);
+        if (i < n) ls.cum[i] = before + x;
+        base += all;
+    }
+    __syncthreads();
+}
 
 // Many candidates are not sorted: they go into TH bins by their key, a thread a bin, and only the bin in which a bound is passed is (4000 candidates: 8 us a bound instead of 30 for
 // all).  base: weight in front of the first candidate.
 struct Picked { u64 mass, w; int index; };   // weight up to and with the candidate, its own, its place in the row
 
-template <typename W>
 struct Fine {
     Shared &sh;
     Lists &ls;
-    const W &w;
+    const Weight &w;
     int n, shift;
     uint32_t hi;
     u64 m, m_before;
     int c, c_before;
     __device__ int bin(u64 cand) const { return (int)((hi - (uint32_t)(cand >> 32)) >> shift); }
-    __device__ Fine(Shared &sh_, Lists &ls_, const W &w_, int n_, u64 base) : sh(sh_), ls(ls_), w(w_), n(n_)
+    __device__ Fine(Shared &sh_, Lists &ls_, const Weight &w_, int n_, u64 base) : sh(sh_), ls(ls_), w(w_), n(n_)
     {
         const int tid = threadIdx.x;
         uint32_t h = 0, l = 0xffffffffu;
@@ -676,25 +679,25 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
         prob = 1.f;
     } else if (top_k || mp > 0.f) {
         // candidates are a first part of the order that holds everything that can be kept
-        const Weigh w{(double)M, cs};
+        const Weigh exact{(double)M, cs};
         const bool by_min = !top_k;
         uint32_t lo;
-        double total = 0.0;
+        u64 row_mass = 0;   // by_min and top_p, which is a share of the whole row: its weight, and what that is held against
+        int ref = 0;
         if (by_min) {
             const double z = (double)M + (double)t * log(fmin((double)mp, 1.0));
             lo = M == INFINITY ? kmax : t == INFINITY ? 0 : key_of((float)(z - (fabs(z) + fabs((double)M)) * 1e-6 - 1e-30));   // a little below: the weights decide
-            if (p < 1.f) {       // top_p is a share of the whole row
+            if (p < 1.f) {
                 const double top = (double)M * cs;
                 done = fabs(top) < Y_MAX - 64.0;
                 if (done) {
-                    const int ref = (int)ceil(top);
-                    u64 m = 0;
+                    if (tid < 64) sh.table[tid] = exp2(tid * (1.0 / 64.0));
+                    ref = (int)ceil(top);
                     for (int c = tid; c < chunks; c += TH) {
                         const int back = ref - ws.ref[(size_t)r * chunks + c];
-                        if (back < 46) m += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + BINS] >> back;
+                        if (back < 46) row_mass += ws.hist[((size_t)r * chunks + c) * (BINS + 1) + BINS] >> back;
                     }
-                    m = block_reduce(sh, m, [](u64 x, u64 y) { return x + y; });
-                    total = (double)m * exp2((double)ref - top);   // relative to the largest weight, as the candidates' are
+                    row_mass = block_reduce(sh, row_mass, [](u64 x, u64 y) { return x + y; });
                 }
             }
         } else {
@@ -703,11 +706,14 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
         }
         done = done && gather(ls, row, keys, per, lo, KEY_INF);
         if (done) {
+            const bool shares = by_min && p < 1.f;
+            const Weight w{cs, shares ? (double)ref : (double)M, shares ? sh.table : nullptr};   // of the sums; a single weight against min_p is always the exact one
             int n = ls.n_cand;
             const double least = fmin((double)mp, 1.0) * ONE;
+            double total = (double)row_mass;
             bool fine = n > SORT_ALL;
             if (fine) {
-                Fine<Weigh> bins(sh, ls, w, n, 0);
+                Fine bins(sh, ls, w, n, 0);
                 Picked at;
                 u64 kept = ~0ull, heavy = 0;
                 if (top_k && k < n) { fine = bins.pick(BY_COUNT, (u64)k, &at); kept = at.mass; }
@@ -718,7 +724,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                     if (bound <= kept) { fine = bins.pick(MASS_AT_LEAST, max(bound, (u64)1), &at); kept = at.mass; }
                 }
                 if (fine && mp > 0.f) {
-                    for (int i = tid; i < n; i += TH) { const u64 x = w(logit_at(ls, i)); heavy += (double)x >= least ? x : 0; }
+                    for (int i = tid; i < n; i += TH) { const float z = logit_at(ls, i); const u64 x = w(z); heavy += (double)(shares ? exact(z) : x) >= least ? x : 0; }
                     kept = min(kept, block_reduce(sh, heavy, [](u64 x, u64 y) { return x + y; }));
                 }
                 if (fine && (fine = bins.pick(MASS_ABOVE, min((u64)(share * (double)kept), kept - 1), &at))) {
@@ -738,7 +744,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                     int l = 1, h = keep;
                     while (l < h) {
                         const int mid = (l + h) >> 1;
-                        if ((double)(ls.cum[mid] - ls.cum[mid - 1]) < least) h = mid; else l = mid + 1;
+                        if ((double)(shares ? exact(logit_at(ls, mid)) : ls.cum[mid] - ls.cum[mid - 1]) < least) h = mid; else l = mid + 1;
                     }
                     keep = h;
                 }
@@ -754,7 +760,8 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
         done = fabs(top) < Y_MAX - 64.0;
         if (done) {
             const int ref = (int)ceil(top);
-            const FromRef w{cs, (double)ref};
+            if (tid < 64) sh.table[tid] = exp2(tid * (1.0 / 64.0));
+            const Weight w{cs, (double)ref, sh.table};
             u64 m = 0, rest = 0, all, rest_all;
             for (int c = tid; c < chunks; c += TH) sh.cnt[c] = (uint32_t)min(ref - ws.ref[(size_t)r * chunks + c], 46);   // octaves that a chunk's weights are moved down; 46: all of it
             __syncthreads();
@@ -771,8 +778,8 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             const u64 before = block_scan(sh, m, &all);
             block_scan(sh, rest, &rest_all);
             const u64 total = all + rest_all;
-            // The bin in which the running weight passes `bound`, and the token of it that does.  The bins' sums are rounded otherwise than the tokens' own, so that a bound just below
-            // the weight that top_p keeps may seem to lie behind the cut's bin: it is the cut's token then, which *p holds.
+            // The bin in which the running weight passes `bound`, and the token of it that does.  A bin of tokens below 2^-14 of the largest may be summed otherwise than the tokens
+            // one by one, so that a bound just below the weight that top_p keeps may seem to lie behind the cut's bin: it is the cut's token then, which *p holds.
             int cut = BINS;
             auto locate = [&](u64 bound, bool above, Picked *p) -> bool {
                 if (tid == 0) sh.hit = -1;
@@ -800,13 +807,13 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                 if (!gather(ls, row, keys, per, lo, hi) || ls.n_cand == 0) return false;
                 const int n = ls.n_cand;
                 if (n > SORT_ALL) {
-                    Fine<FromRef> bins(sh, ls, w, n, base);
+                    Fine bins(sh, ls, w, n, base);
                     if (bins.pick(above ? MASS_ABOVE : MASS_AT_LEAST, bound, p)) return true;
                     __syncthreads();
                 }
                 sort(ls.cand, n);
                 weigh(sh, ls, n, base, w);
-                const int at = min(first_past(ls, n, bound, above), n - 1);   // the bin's sum is rounded otherwise than its parts: at most the last
+                const int at = min(first_past(ls, n, bound, above), n - 1);   // (as above) at most the last
                 *p = Picked{ls.cum[at], w(logit_at(ls, at)), index_at(ls, at)};
                 return true;
             };

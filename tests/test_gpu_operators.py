@@ -76,6 +76,26 @@ def test_sample_ties(dtype, values):
         check_sample(z, 1.0, k, p, 0.0, rng.random(6))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,equal", [(2, 2), (4, 4), (64, 64), (1024, 1024), (4096, 4096), (8192, 8192), (20011, 8), (152064, 16), (60000, 256)])
+def test_sample_bounds_between_equal_tokens(V, equal, dtype):
+    """Shares and numbers that are a whole number of equal tokens, exactly: the bound belongs to the token in front of it for top_p, and to the one behind it for u.  The tokens stand all over the
+    row, among others without weight, so that parts of the row are held against other powers of two."""
+    rng = np.random.default_rng(V)
+    R = 16
+    z = torch.full((R, V), -math.inf)
+    for r in range(R):
+        c = float(rng.normal()) * 7
+        if r % 2:
+            z[r] = c - 90.0 * (1 + torch.rand(V, generator=torch.Generator().manual_seed(r)))
+        z[r, torch.from_numpy(rng.permutation(V)[:equal])] = c
+    z = z.to(DT[dtype]).cuda()
+    t = rng.uniform(0.3, 1.4, R)
+    u = rng.integers(0, equal, R) / equal
+    for k, p, m in [(0, 1.0, 0.0), (0, 0.5, 0.0), (0, 0.25, 0.0), (0, 0.75, 0.5), (0, 1.0, 0.5), (equal, 0.5, 0.0), (equal, 1.0, 0.0)]:
+        check_sample(z, t, k, p, m, u)
+
+
 def test_sample_masks_and_non_finite():
     V, inf, nan = 5003, math.inf, math.nan
     z = torch.randn(10, V, generator=torch.Generator().manual_seed(3))
