@@ -140,6 +140,15 @@ def test_sample_draws_in_front_of_cuts(V, spread, dtype):
     check_sample(z.repeat(96, 1).contiguous(), 1.2, 0, rng.permutation(np.linspace(0.2, 0.995, 96)), 0.0, u)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [2049, 4000, 9001, 152064])
+def test_sample_wide_top_k(V, dtype):
+    """Around the largest top_k that goes by candidates, also where more logits reach its bound than can be held (bf16: many equal ones)."""
+    z, rng = draw_logits(V, 4, V, dtype, spread=1.2)
+    for k in (1023, 1024, 1025, 2047, 2048, 2049, 4000):
+        check_sample(z, 1.0, k, rng.choice([1.0, 0.9], 4), 0.0, rng.random(4))
+
+
 @pytest.mark.parametrize("V", [3001, 50021])
 def test_sample_of_the_last_kept_token(V):
     """u = 1 is the last token that top_p keeps, whatever the bins' rounded sums are: 64 cuts of a row."""
