@@ -9,12 +9,13 @@
 //   - top-k: the k-th largest of the runs' maxima is no more than the k-th largest logit, so the candidates are what reaches it, in the few runs that do;
 //   - min-p: the candidates are what reaches min_p of the largest;
 //   - otherwise the histogram says in which bin the weight passes top_p, and in which bin the draw falls, and the candidates are that bin.
-// Where the candidates do not fit (thousands of equal logits), where top-k is beyond TOP_MAX in a longer row than can be held, or where the exponents leave the histogram's range, the row is searched by digits
+// Where a row has too few runs for its top-k, the k-th logit itself is searched by digits.  Where the candidates do not fit (thousands of equal logits, top-k beyond CAND), or where the exponents leave the histogram's range, the row is searched by digits
 // of the logits' order-preserving integers instead, without sorting, in a dozen passes.
 //
 // us: one row of 151936 fp32 5 + 13, 256 rows of 152064 with mixed settings 51 + 46, 33 rows of 33003 bf16 13 + 28.  The first launch is bound by the read where no row asks for weights (256 rows 39, 4.0 TB/s),
 // else by the weights' instructions.  The second is a chain of scans and synchronisations in one workgroup, whose longest part, where a bound lies far down a flat tail, is the read of the whole row (about
-// 25 each time, by its instructions).  256 rows with top_k = 2048 86, and 5000, by digits: 760.
+// 25 each time, by its instructions).  256 rows with top_k = 2048 86, 4000 (the k-th by digits) 368, 5000 (all by digits) 760; 36 rows of 7452 bf16 with
+// top_k = 1000, which have fewer runs than that, 66 (by digits 108).
 #include "ops.hpp"
 
 namespace sdlm {
@@ -208,7 +209,7 @@ __device__ void by_digits(Shared &sh, const Row<T> &row, float M, float t, int k
 constexpr int PER_THREAD = 64, CHUNK = 256 * PER_THREAD;   // logits of a thread and of a workgroup
 constexpr int RUNS = 9;                        // runs of a thread of the second launch, at most: the largest vocabulary has (524288 + 7) / 64
 constexpr int OCTAVES = 24, PER_OCTAVE = 32, BINS = OCTAVES * PER_OCTAVE, COPIES = 4;   // the last bin, BINS: all below
-constexpr int TOP_MAX = 2048;                  // largest top-k that goes by candidates: beyond, a long row has too few runs, so that more reach the bound than can be held
+constexpr int TOP_MAX = 2048;                  // largest top-k whose bound is taken from the runs of a long row: beyond, so many logits reach it that they cannot be held
 constexpr double Y_MAX = 16384.0;              // largest exponent (of 2) whose fraction keeps 39 bits
 
 // What a row's settings ask of the first launch.
@@ -701,10 +702,16 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
                 }
             }
         } else {
-            done = k <= TOP_MAX || row.V <= CAND;
-            lo = done ? kth_run(sh, keys, k) : 0;
+            done = k <= CAND;
+            lo = k <= TOP_MAX || row.V <= CAND ? kth_run(sh, keys, k) : KEY_INF + 1;
         }
-        done = done && gather(ls, row, keys, per, lo, KEY_INF);
+        if (done) {
+            done = lo <= KEY_INF && gather(ls, row, keys, per, lo, KEY_INF);
+            if (!done && top_k) {   // too few runs for a bound (a short row, or few tokens above -infinity), or too many equal logits near it: the k-th itself
+                __syncthreads();
+                done = gather(ls, row, keys, per, search(sh, plain, exact, BY_COUNT, (u64)k).key, KEY_INF);
+            }
+        }
         if (done) {
             const bool shares = by_min && p < 1.f;
             const Weight w{cs, shares ? (double)ref : (double)M, shares ? sh.table : nullptr};   // of the sums; a single weight against min_p is always the exact one
