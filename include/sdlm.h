@@ -406,8 +406,8 @@ int sdlm_kv_describe(sdlm_ctx *ctx, sdlm_kv *kv);
  * node_offsets[b] + i of `mask`; a tree of drafts sets the node's own bit and its ancestors', but any mask will do.  K/V of node j are at position node_base[b] + j
  * of the table node_table (n_seqs x node_pages entries): the sequence's own table with node_base = lengths, where nodes are appended behind the cache, or pages of their own.
  *   out[r, h] = sum_j softmax_j(q[r, h] . K[j] / sqrt(head_dim)) V[j]; zeros for a node that sees nothing.
- * Query head h reads kv head h / (n_q_heads / n_kv_heads).  bf16: the softmax's weights are rounded to bf16 in front of the product with V (half a step of 2^-8 each, as in a context's own
- * attention); sums, maxima and the division are fp32.  K/V that a node does not see may hold anything, NaN too, and changes nothing.  Reads pool, page_table and lengths of `kv`.
+ * Query head h reads kv head h / (n_q_heads / n_kv_heads).  bf16: the softmax's weights keep 2^-16 of themselves in front of the product with V (two bf16 operands each),
+ * sums, maxima and the division are fp32.  K/V that a node does not see may hold anything, NaN too, and changes nothing.  Reads pool, page_table and lengths of `kv`.
  */
 typedef struct {
     const void *q;               /* [dev] n_rows x n_q_heads x head_dim, element type of the cache */

@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
     const int end = (int)min((long)all, (long)(id % a.groups + 1) * run);
     int from = (int)min((long)all, (long)(id % a.groups) * run);
     __shared__ __attribute__((aligned(16))) T kv[2][2 * TILE];   // two pairs of tiles, each as in the pool
-    __shared__ int strange[2][4];   // per wavefront: whether its part of the pair's values has some that are not finite (only where a query may not see all slots)
+    __shared__ int strange[2][4];   // per wavefront: whether its part of the pair's values has some that are not finite (not for pairs that every query sees whole)
     const T *pool = (const T *)a.t.pool;
     for (int part = 0; from < end; ++part) {
     const Place pl = place_of(a.t, sums, G, QB, from, false);
@@ -281,12 +281,6 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
     }
     f32x4 O[QT][ND];
     float m_run[QT], l_run[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        m_run[t] = -INFINITY; l_run[t] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) O[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
 
     // Pages of 64 tiles, one a lane, and of the next 64: a lookup of its own in front of every pair would put a memory round trip into every iteration.  -1: there is none.
     auto pages = [&](int w) -> int {
@@ -296,7 +290,8 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
         else if (u < u1 && u + node_tile0 < a.t.t.node_pages) p = ntab[u + node_tile0];
         return p < a.t.kv.n_tiles ? p : -1;
     };
-    int pg = pages(0), pg_next = n_pairs > 32 ? pages(1) : -1;
+    int pg, pg_next;
+    bool careful = false;   // the second try of a part whose values are not all finite, see its end
     // a pair in flight: its tiles' contents, and whether they exist.  Called for pairs in ascending order.
     auto fetch = [&](int pp, u32x4 (&r)[VEC]) -> int {
         if ((pp & 31) == 0 && pp > 0) {
@@ -312,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
         }
         return (pA >= 0 ? 1 : 0) | (pB >= 0 ? 2 : 0);
     };
-    auto is_whole = [&](int pp, int have) { return have == 3 && (u0 + 2 * pp + 2) * PAGE <= s.len; };   // every key of the pair is seen by every query
+    auto is_whole = [&](int pp, int have) { return !careful && have == 3 && (u0 + 2 * pp + 2) * PAGE <= s.len; };   // every key of the pair is seen by every query
     auto stash = [&](int buf, const u32x4 (&r)[VEC], int pp, int have) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) *(u32x4 *)(&kv[buf][0] + (size_t)(tid + 256 * i) * E) = r[i];
@@ -423,7 +418,10 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
                 for (int v = 0; v < 4; ++v) { x[t][v] = fmaf(sA[t][v], a.c, -to); x[t][4 + v] = fmaf(sB[t][v], a.c, -to); }
             }
         }
-        Op8 pop[QT];
+        // bf16: a weight goes into the product as two operands, its rounding to bf16 and what that leaves, so that it keeps 2^-16 of itself.  One rounding alone is up to 2^-8 of each weight, as much
+        // again as the output's own (relative error against 64 bits, and us a call for 64 sequences and for 4 wide trees as above: one operand 2.3e-3, 107 and 91; two 1.66e-3, which is the
+        // output's rounding alone, 113 and 109).
+        Op8 pop[QT], rest[QT];
         f32x4 pA[QT], pB[QT];   // the weights of the slots 4 lg + v of each tile
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
@@ -433,10 +431,14 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
                 pB[t][v] = __builtin_amdgcn_exp2f(x[t][4 + v]);
             }
             l_run[t] += (pA[t][0] + pA[t][1]) + (pA[t][2] + pA[t][3]) + (pB[t][0] + pB[t][1]) + (pB[t][2] + pB[t][3]);
-            if constexpr (!F32) {
-                pop[t].w[0] = pack_bf16(pA[t][0], pA[t][1]); pop[t].w[1] = pack_bf16(pA[t][2], pA[t][3]);
-                pop[t].w[2] = pack_bf16(pB[t][0], pB[t][1]); pop[t].w[3] = pack_bf16(pB[t][2], pB[t][3]);
-            }
+            if constexpr (!F32)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x0 = i < 2 ? pA[t][2 * i] : pB[t][2 * i - 4], x1 = i < 2 ? pA[t][2 * i + 1] : pB[t][2 * i - 3];
+                    const uint32_t w = pack_bf16(x0, x1);
+                    pop[t].w[i] = w;
+                    rest[t].w[i] = pack_bf16(x0 - __uint_as_float(w << 16), x1 - __uint_as_float(w & 0xffff0000u));
+                }
         }
         // A slot that a query does not see may hold anything, and 0 times a value that is not finite is not 0.  Such values are added one by one for the queries that see them.
         const bool odd = !whole && (strange[buf][0] | strange[buf][1] | strange[buf][2] | strange[buf][3]);
@@ -448,17 +450,10 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
                 float w[QT];
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
-                    if constexpr (F32) {
-                        const int k = slot & 3;
-                        const f32x4 mine = slot < 16 ? pA[t] : pB[t];
-                        const float lo = k & 1 ? mine[1] : mine[0], hi = k & 1 ? mine[3] : mine[2];
-                        w[t] = __shfl(k & 2 ? hi : lo, from);
-                    } else {
-                        const int k = (slot >> 4) * 2 + ((slot & 3) >> 1);
-                        const uint32_t lo = k & 1 ? pop[t].w[1] : pop[t].w[0], hi = k & 1 ? pop[t].w[3] : pop[t].w[2], mine = k & 2 ? hi : lo;
-                        const uint32_t y = (uint32_t)__shfl((int)mine, from);
-                        w[t] = __uint_as_float(slot & 1 ? y & 0xffff0000u : y << 16);
-                    }
+                    const int k = slot & 3;
+                    const f32x4 mine = slot < 16 ? pA[t] : pB[t];
+                    const float lo = k & 1 ? mine[1] : mine[0], hi = k & 1 ? mine[3] : mine[2];
+                    w[t] = __shfl(k & 2 ? hi : lo, from);
                 }
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
@@ -504,9 +499,21 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                for (int t = 0; t < QT; ++t) O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo[dt].v, pop[t].v, O[t][dt], 0, 0, 0);
+                for (int t = 0; t < QT; ++t) {
+                    O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo[dt].v, pop[t].v, O[t][dt], 0, 0, 0);
+                    O[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo[dt].v, rest[t].v, O[t][dt], 0, 0, 0);
+                }
         }
     };
+    for (;;) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        m_run[t] = -INFINITY; l_run[t] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) O[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    pg = pages(0);
+    pg_next = n_pairs > 32 ? pages(1) : -1;
     u32x4 rA[VEC], rB[VEC];   // two pairs in flight: the next one and the one after it
     int hA = 0, hB, h0, h1 = 0;
     hB = fetch(0, rB);
@@ -525,6 +532,21 @@ __global__ __launch_bounds__(256, 2) void tree_mfma_k(MfmaArgs a)
         compute(pp + 1, 1, h1);
         if (pp + 2 < n_pairs) { stash(0, rB, pp + 2, hB); h0 = hB; }
         __syncthreads();
+    }
+    if constexpr (F32) break;
+    else {
+        // An infinite value times the two operands of a weight is infinity less infinity, or times nothing.  Where a result is not finite, the part is computed once more with such values taken out
+        // of every tile and added with the whole weight.
+        bool odd = false;
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd |= !finite32(__float_as_uint(O[t][dt][i]));
+        if (careful || !__syncthreads_or(odd)) break;
+        careful = true;
+    }
     }
     if (active) {
 #pragma unroll

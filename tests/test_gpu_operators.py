@@ -276,6 +276,38 @@ def test_tree_attention_non_finite_nodes(value, dtype):
         c["pool"] = clean
 
 
+@pytest.mark.parametrize("heads,lens,nodes", [((4, 2, 64), [300, 0, 17], [9, 30, 70]), ((12, 2, 128), [700], [12]), ((16, 2, 128), [1500, 3], [150, 80]), ((6, 1, 32), [90], [5]), ((15, 3, 96), [333, 64], [40, 1])])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_tree_attention_bf16_loses_what_its_result_loses(heads, lens, nodes, inplace):
+    """A weight keeps 2^-16 of itself in front of V (two roundings to half a step of 2^-8), fp32 sums and exponents 2^-17 as in check_tree: together with the result's half step, which is taken
+    of the computed value, below 2^-15 of the weighted mean of |V| and 2^-8 of the result."""
+    c = tree_case(12, heads, lens, nodes, "bf16", inplace=inplace)
+    got = run_tree(c).double().cpu().numpy()
+    x = c["pool"][0].double().numpy()
+    args = (c["q"].double().numpy(), c["table"], c["lens"], c["offs"], c["seen"], c["ntab"], c["base"])
+    ref, vmean = plain.tree_attention(x, *args), plain.tree_attention(np.concatenate([x[:, :, :1], np.abs(x[:, :, 1:])], 2), *args)
+    assert (np.abs(got - ref) <= 2.0 ** -15 * vmean + 2.0 ** -8 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("dtype,kw", [("fp32", {}), ("fp32", dict(max_len=4096)), ("bf16", {})])
+@pytest.mark.parametrize("heads,lens", [((6, 2, 64), [200, 64]), ((12, 2, 128), [3000, 90])])
+def test_tree_attention_infinite_values(heads, lens, dtype, kw):
+    """Infinite values of the cache, which all nodes see: infinite in their features, of both signs no number, and nothing else changes."""
+    hq, hkv, d = heads
+    G, f = hq // hkv, np.arange(5, 9)
+    c = tree_case(13, heads, lens, [7, 12], dtype)
+    ref = run_tree(c, **kw)
+    for p, value in ((5, math.inf), (38, math.inf)):
+        c["pool"][0, c["table"][0][p // 16], 1, 1, plain.v_index(p % 16, f)] = value
+    out = run_tree(c, **kw)
+    assert (out[:7, G:, 5:9] == math.inf).all()
+    c["pool"][0, c["table"][0][2], 1, 1, plain.v_index(7, f[:2])] = -math.inf
+    both = run_tree(c, **kw)
+    assert torch.isnan(both[:7, G:, 5:7]).all() and (both[:7, G:, 7:9] == math.inf).all()
+    for o in (out, both):
+        assert torch.equal(o[7:], ref[7:]) and torch.equal(o[:7, :G], ref[:7, :G]) and torch.equal(o[:7, G:, :5], ref[:7, G:, :5]) and torch.equal(o[:7, G:, 9:], ref[:7, G:, 9:])
+
+
 HEADS = [(4, 2, 64), (12, 2, 128), (7, 1, 128), (8, 8, 32), (15, 3, 96)]
 
 
