@@ -405,7 +405,7 @@ int sdlm_kv_describe(sdlm_ctx *ctx, sdlm_kv *kv);
  * (at most max_nodes; further rows are left alone).  Node i of b sees the positions 0 .. lengths[b]-1 of the cache and those nodes j of b whose bit (word j / 64, bit j % 64) is set in row
  * node_offsets[b] + i of `mask`; a tree of drafts sets the node's own bit and its ancestors', but any mask will do.  K/V of node j are at position node_base[b] + j
  * of the table node_table (n_seqs x node_pages entries): the sequence's own table with node_base = lengths, where nodes are appended behind the cache, or pages of their own.
- *   out[r, h] = sum_j softmax_j(q[r, h] . K[j] / sqrt(head_dim)) V[j]; zeros for a node that sees nothing.
+ *   out[r, h] = sum_j softmax_j(q[r, h] . K[j] / sqrt(head_dim)) V[j]; zeros for a node that sees nothing, or scores of -infinity only.
  * Query head h reads kv head h / (n_q_heads / n_kv_heads).  bf16: the softmax's weights keep 2^-16 of themselves in front of the product with V (two bf16 operands each),
  * sums, maxima and the division are fp32.  K/V that a node does not see may hold anything, NaN too, and changes nothing.  Reads pool, page_table and lengths of `kv`.
  */

@@ -75,7 +75,8 @@ __global__ __launch_bounds__(256) void tree_rows_k(TreeArgs a)
         }
         float mx = s;
         for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-        const float mn = fmaxf(m, mx), corr = m == -INFINITY ? 0.f : __expf(m - mn), p = vis ? __expf(s - mn) : 0.f;   // a NaN score stays one, whatever mn is
+        const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;   // scores of -infinity weigh nothing, also where there are no others yet
+        const float corr = m == -INFINITY ? 0.f : __expf(m - ref), p = vis ? __expf(s - ref) : 0.f;   // a NaN score stays one, whatever ref is
         m = mn;
         l = l * corr + p;
 #pragma unroll

@@ -308,6 +308,38 @@ def test_tree_attention_infinite_values(heads, lens, dtype, kw):
         assert torch.equal(o[7:], ref[7:]) and torch.equal(o[:7, :G], ref[:7, :G]) and torch.equal(o[:7, G:, :5], ref[:7, G:, :5]) and torch.equal(o[:7, G:, 9:], ref[:7, G:, 9:])
 
 
+@pytest.mark.parametrize("dtype,kw", [("fp32", {}), ("fp32", dict(max_len=4096)), ("bf16", {})])
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+def test_tree_attention_infinite_scores(value, dtype, kw):
+    """A score of -infinity weighs nothing, wherever such keys stand: in all of a launch's first tiles, alone, among the nodes; a row that sees no other key is zero.  Of +infinity: no numbers."""
+    c = tree_case(11, (4, 2, 64), [200, 70, 0], [5, 9, 20], dtype)
+    c["q"][:, :, 3] = c["q"][:, :, 3].abs() + 0.5
+    if value > 0:
+        c["q"][:, :, 3] *= -1
+    clean, ref, f = c["pool"].clone(), run_tree(c, **kw), np.array([3])
+    for b, keys in ((0, [*range(64), 100, *range(130, 200)]), (1, range(70))):      # of kv head 0
+        for p in keys:
+            c["pool"][0, c["table"][b][p // 16], 0, 0, plain.k_index(p % 16, f)] = value
+    c["pool"][0, c["ntab"][2][0], 0, 0, plain.k_index(0, f)] = value                # a first node, which sees itself alone
+    out = run_tree(c, **kw)
+    assert torch.equal(out[:, 2:], ref[:, 2:])
+    assert (out[c["offs"][2], :2] == 0).all()
+    x = c["pool"][0].double().numpy()
+    args = (c["q"].double().numpy(), c["table"], c["lens"], c["offs"], c["seen"], c["ntab"], c["base"])
+    with np.errstate(invalid="ignore"):
+        want = plain.tree_attention(x, *args)
+        vmean = plain.tree_attention(np.concatenate([x[:, :, :1], np.abs(x[:, :, 1:])], 2), *args)
+    want[c["offs"][2], :2] = vmean[c["offs"][2], :2] = 0.0
+    step = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24 * 128      # as in check_tree
+    got = out.double().cpu().numpy()
+    assert np.isfinite(want).all() and np.isfinite(got).all()
+    assert (np.abs(got - want) <= step * vmean + step * np.abs(want) + 1e-30).all()
+    c["pool"] = clean
+    c["pool"][0, c["table"][0][7], 0, 0, plain.k_index(4, f)] = -value
+    out = run_tree(c, **kw)
+    assert torch.isnan(out[:5, :2]).all() and torch.equal(out[:, 2:], ref[:, 2:]) and torch.equal(out[5:], ref[5:])
+
+
 HEADS = [(4, 2, 64), (12, 2, 128), (7, 1, 128), (8, 8, 32), (15, 3, 96)]
 
 
