@@ -353,7 +353,7 @@ const char *sdlm_op_error(void);
  * w = exp((z - max z) / temperature) a token is kept while
  *   - it is among the first top_k (top_k <= 0: all), and
  *   - the weight of those before it, as a share of the first top_k together, is below top_p (top_p >= 1 or NaN: all), and
- *   - w >= min_p (min_p <= 0 or NaN: all);
+ *   - w >= min_p (min_p <= 0 or NaN: all; above 1: none);
  * the first is always kept.  Drawn is the first kept token, in that order, whose running weight exceeds u times the weight of all kept ones.  A temperature <= 0 (or NaN)
  * draws the first.  Where the largest logit is +infinity, only the tokens with it have weight.  A row without any token above -infinity gives id -1 and probability 0.
  * Weights are held to 2^-45 of the largest, and where the whole row counts (no top_k) to 2^-30 of themselves, in integers, equal ones for equal logits: a result does not depend on the launch or on the row's neighbours.  A token whose weight is below that is not drawn.

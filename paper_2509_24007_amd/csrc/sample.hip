@@ -187,7 +187,7 @@ __device__ void by_digits(Shared &sh, const Row<T> &row, float M, float t, int k
     const Weigh w{(double)M, LOG2E / (double)t};
     auto add = [](u64 x, u64 y) { return x + y; };
     u64 n = 0, m = 0, mm = 0;
-    const double least = fmin((double)mp, 1.0) * ONE;
+    const double least = (double)mp * ONE;
     for (int i = threadIdx.x; i < row.V; i += TH) {
         const float z = row.at(i);
         const u64 x = z == -INFINITY ? 0 : w(z);
@@ -217,7 +217,7 @@ __device__ inline bool wants_weights(const sdlm_sample_args &a, int r)
 {
     const float t = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
     const int k = a.top_k ? a.top_k[r] : 0;
-    return t > 0.f && (k <= 0 || k >= a.vocab) && !(mp > 0.f && !(p < 1.f));
+    return t > 0.f && !(mp > 1.f) && (k <= 0 || k >= a.vocab) && !(mp > 0.f && !(p < 1.f));
 }
 
 // ... of which min-p needs the sum alone.
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
     const bool top_k = k > 0 && k < row.V;
     if (M == -INFINITY) {
         // every token is masked
-    } else if (!(t > 0.f)) {
+    } else if (!(t > 0.f) || mp > 1.f) {   // the first token: no weight reaches a min_p above 1
         if ((done = gather(ls, row, keys, per, kmax, kmax))) {
             u64 best = 0;
             for (int i = tid; i < ls.n_cand; i += TH) best = max(best, ls.cand[i]);
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
         u64 row_mass = 0;   // by_min and top_p, which is a share of the whole row: its weight, and what that is held against
         int ref = 0;
         if (by_min) {
-            const double z = (double)M + (double)t * log(fmin((double)mp, 1.0));
+            const double z = (double)M + (double)t * log((double)mp);
             lo = M == INFINITY ? kmax : t == INFINITY ? 0 : key_of((float)(z - (fabs(z) + fabs((double)M)) * 1e-6 - 1e-30));   // a little below: the weights decide
             if (p < 1.f) {
                 const double top = (double)M * cs;
@@ -716,7 +716,7 @@ __global__ __launch_bounds__(TH) void sample_draw_k(sdlm_sample_args a, SampleWs
             const bool shares = by_min && p < 1.f;
             const Weight w{cs, shares ? (double)ref : (double)M, shares ? sh.table : nullptr};   // of the sums; a single weight against min_p is always the exact one
             int n = ls.n_cand;
-            const double least = fmin((double)mp, 1.0) * ONE;
+            const double least = (double)mp * ONE;
             double total = (double)row_mass;
             bool fine = n > SORT_ALL;
             if (fine) {

@@ -156,6 +156,25 @@ def test_sample_of_the_last_kept_token(V):
     check_sample(z, 1.0, 0, np.linspace(0.3, 0.999, 64), 0.0, 1.0)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1, 300, 5003, 152064])
+def test_sample_min_p_above_one(V, dtype):
+    """No weight reaches a min_p above 1, not the largest itself: the first token alone is kept, also where others are equal to it.  At 1 those are."""
+    z, rng = draw_logits(V, 5, V, dtype)
+    at = np.sort(rng.permutation(V)[:4])
+    z[:, torch.from_numpy(at).cuda()] = 40.0
+    z[3] = -math.inf
+    z[4, torch.from_numpy(at).cuda()] = math.inf
+    first = [int(at[0])] * 3 + [-1, int(at[0])]
+    for t in (0.8, math.inf):
+        for k, p in [(0, 1.0), (0, 0.7), (3, 1.0), (100, 0.9), (5000, 0.4)]:
+            for m in (float(np.float32(1) + np.float32(2.0 ** -23)), 1.5, math.inf):
+                full = functools.partial(torch.full, (5,), device="cuda")
+                ids, prob = sdlm.sample(z, dev(rng.random(5), torch.float32), temperature=full(t), top_k=full(k, dtype=torch.int32), top_p=full(p), min_p=full(m))
+                assert ids.cpu().tolist() == first and prob.cpu().tolist() == [1.0, 1.0, 1.0, 0.0, 1.0], (t, k, p, m)
+    check_sample(z[:3], 0.8, 0, 1.0, 1.0, [0.1, 0.6, 0.9])
+
+
 def test_sample_uniform_out_of_range_and_defaults():
     z, _ = draw_logits(2, 4, 999, "fp32")
     check_sample(z, 1.0, 0, 1.0, 0.0, [-1.0, 1.0, 7.0, 0.25])
