@@ -15,6 +15,7 @@ void launch_sample(hipStream_t s, const sdlm_sample_args &a, void *workspace);
 constexpr int TREE_MAX_NODES = 1024;
 bool tree_fits(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes);   // the launch's counters hold them
 size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes, int max_len);
+size_t tree_workspace_least(int n_kv_heads, int head_dim, int dtype);   // what launch_tree_attention needs at least, whatever the sizes of the call are
 void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sdlm_tree_args &t, void *workspace, size_t workspace_bytes);
 
 // ---- pages (kv_pages.hip)

@@ -176,8 +176,11 @@ void plan(const sdlm_model_cfg *m, const sdlm_run_cfg *r, Layout *L)
     L->tree_ints = (size_t)B * (TREE_NODES * 3 + 3 + 1 + D) + 1 + 8;
     L->tree_i32 = take(L->tree_ints * 4);
     L->tree_mask = take((size_t)L->tree_rows * TREE_WORDS * 8);
-    L->tree_ws_bytes = L->mfma ? L->slab_floats * 4 : (size_t)8 << 20;   // matrix-core path: the split-k slabs, free during the attention
-    L->tree_ws = L->mfma ? L->slabs : take(L->tree_ws_bytes);
+    // what the attention cannot do without (a run of work for each kv head), and otherwise 8 MB; on the matrix-core path the split-k slabs, free while it runs, if they hold it
+    const size_t tree_least = tree_workspace_least(m->n_kv_heads, m->head_dim, m->dtype), slab_bytes = L->slab_floats * 4;
+    const bool in_slabs = L->mfma && slab_bytes >= tree_least;
+    L->tree_ws_bytes = in_slabs ? slab_bytes : std::max((size_t)8 << 20, tree_least);
+    L->tree_ws = in_slabs ? L->slabs : take(L->tree_ws_bytes);
     L->total = o;
 }
 

@@ -642,6 +642,9 @@ Shape shape_of(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
     return s;
 }
 
+// The places for the parts of one workgroup of each kv head.
+size_t run_bytes(int n_kv_heads, int head_dim, int qt) { return (size_t)n_kv_heads * 2 * 64 * qt * (head_dim * 4 + 8); }
+
 template <typename T, int HD, int QT>
 void mfma_go(hipStream_t s, const MfmaArgs &a, const Shape &sh)
 {
@@ -680,8 +683,10 @@ bool tree_fits(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes)
 size_t tree_workspace_bytes(const sdlm_kv &kv, int n_q_heads, int n_seqs, int max_nodes, int max_len)
 {
     const Shape sh = shape_of(kv, n_q_heads, n_seqs, max_nodes);
-    return (size_t)sh.groups * kv.n_kv_heads * 2 * 64 * sh.qt * (kv.head_dim * 4 + 8) + 256;
+    return sh.groups * run_bytes(kv.n_kv_heads, kv.head_dim, sh.qt) + 256;
 }
+
+size_t tree_workspace_least(int n_kv_heads, int head_dim, int dtype) { return run_bytes(n_kv_heads, head_dim, dtype == 0 ? 1 : 2) + 256; }
 
 void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sdlm_tree_args &t, void *workspace, size_t workspace_bytes)
 {
@@ -696,8 +701,8 @@ void launch_tree_attention(hipStream_t s, const sdlm_kv &kv, int layer, const sd
     m.c = 1.4426950408889634f / sqrtf((float)kv.head_dim);
     Shape sh = shape_of(kv, t.n_q_heads, t.n_seqs, t.max_nodes);
     // A context lends less workspace than a caller has to: fewer, longer runs.
-    const long fit = (long)((workspace_bytes - 256) / ((size_t)kv.n_kv_heads * 2 * 64 * sh.qt * (kv.head_dim * 4 + 8)));
-    if (fit < sh.groups) sh.groups = fit < 1 ? 1 : (int)fit;
+    const size_t fit = (workspace_bytes - 256) / run_bytes(kv.n_kv_heads, kv.head_dim, sh.qt);   // at least 1: tree_workspace_least
+    if (fit < (size_t)sh.groups) sh.groups = (int)fit;
     m.part_o = (float *)workspace;
     m.part_ml = (float2 *)((char *)workspace + (size_t)sh.groups * kv.n_kv_heads * 2 * 64 * sh.qt * kv.head_dim * 4);
     m.groups = sh.groups;

@@ -269,6 +269,21 @@ def test_verified_trees(kind, D, T, paged):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,d", [(160, 128), (600, 32)])
+def test_trees_of_many_kv_heads(heads, d, monkeypatch):
+    """More kv heads than 8 MB of partial results hold, and more rows than the small launch takes."""
+    monkeypatch.setitem(MODELS, "wide", (small_cfg(hidden=64, n_q_heads=heads, n_kv_heads=heads, head_dim=d, ffn=112, vocab=300, n_layers=1), 0.1, 1e-4))
+    ctx, om, m, tol, hist = setup("wide", [70], 4, max_batch=1)
+    st = check_history(ctx, om, m, tol, hist)
+    tokens, parents = grow(ctx, m, st, 1, 12, np.random.default_rng(2))
+    z = torch.zeros(1, 12, m.vocab, device="cuda")
+    ctx.verify_tree(torch.from_numpy(tokens).cuda(), torch.from_numpy(parents).cuda(), logits=z)
+    for i in range(0, 12, 3):
+        ref = node_logits(om, hist[0], tokens[0], parents[0], i, 4)
+        assert np.max(np.abs(z[0, i].cpu().numpy() - ref)) / np.max(np.abs(ref)) <= tol
+    ctx.close()
+
+
 @pytest.mark.parametrize("kind", ["fp32", "mfma"])
 def test_trees_of_the_causal_block(kind):
     ctx, om, m, tol, hist = setup(kind, [20, 9, 30], 4, causal=True)

@@ -106,6 +106,15 @@ def test_tree_attention_layer_and_workspace():
     assert L.sdlm_tree_attention(C.byref(kv()), 0, C.byref(tree(n_rows=0)), None, 0, None) == 0
 
 
+@pytest.mark.parametrize("dtype,d,heads", [(0, 128, 600), (0, 32, 900), (1, 64, 400), (1, 128, 1200)])
+def test_a_context_lends_the_trees_a_run_of_every_kv_head(dtype, d, heads):
+    """Beyond a fixed room, a further kv head takes the places of a run's two parts as well: 64 queries (bf16: 128) with a sum of d and two numbers each."""
+    def total(h):
+        m = sdlm.ModelCfg(1, 64, h, h, d, 64, 300, 1e4, 1e-6, 1.0, dtype, 299, 0, 0)
+        return sdlm.load().sdlm_workspace_bytes(C.byref(m), C.byref(sdlm.RunCfg(1, 64, 4, 0, 16, 0, 0.5, 0, 0, 32)))
+    assert total(heads + 2) - total(heads) >= total(12) - total(10) + 2 * 2 * 64 * (1 + dtype) * (4 * d + 8)
+
+
 BIG = 1 << 50      # a layer stride that holds anything
 
 
