@@ -510,6 +510,8 @@ class KvCache:
                            _ints(page_table, S * pps, "page_table", dev), _ints(lengths, S, "lengths", dev), _ints(backed, S, "backed", dev),
                            _ints(page_refs, n_pages, "page_refs", dev), _ints(free_pages, n_pages, "free_pages", dev), _ints(free_count, 1, "free_count", dev))
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(dev).synchronize()   # a fork may run on any stream
 
     def fork(self, parent: torch.Tensor, *, share: bool = True) -> None:
         """Sequence b becomes what sequence parent[b] is (-1: empty); see sdlm_kv_fork.  Does not synchronise: check() raises if the last fork was refused."""
@@ -519,7 +521,8 @@ class KvCache:
         _run_op(self.device, L.sdlm_kv_fork, C.byref(self.desc), _ints(parent, 0, "parent", self.device), parent.numel(), int(share), self.status.data_ptr(), ws.data_ptr(), need)
 
     def check(self) -> None:
-        """Synchronise and raise if the last fork was refused."""
+        """Wait for the device, whatever stream the last fork runs on, and raise if it was refused."""
+        torch.cuda.synchronize(self.device)
         bad = int(self.status.item())
         if bad & 2:
             raise SdlmError(EINVAL, "a parent or a page of the table is out of range: nothing was changed")

@@ -723,6 +723,25 @@ def test_replays_of_captured_calls():
             assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i])), (n, i)
 
 
+@pytest.mark.parametrize("busy", ["the fork's stream", "the cache's"])
+def test_a_refusal_on_another_stream_is_seen(busy):
+    """check() raises for a fork on a stream of its own: one that has not run yet, and one that runs while the stream on which the cache was described is still at other work."""
+    c = cache_case(6, [100, 30, 1], [0, 0, 0], 12)
+    kv, pool, t = kv_of(c)
+    parent, side, x = dev([0, 0, 0]), torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side if busy == "the fork's stream" else torch.cuda.current_stream()):
+        for _ in range(40):       # tens of milliseconds
+            x = (x @ x).tanh_()
+    if busy == "the cache's":
+        kv = sdlm.KvCache(pool, n_pages=12, **t)
+    with torch.cuda.stream(side):
+        kv.fork(parent, share=False)
+    with pytest.raises(sdlm.SdlmError) as e:
+        kv.check()
+    assert e.value.code == sdlm.ECAPACITY
+
+
 def test_a_captured_fork():
     """A fork in a graph, replayed on a cache that changes in between."""
     kv, pool, t, args, _ = round_inputs(51)
