@@ -397,7 +397,8 @@ typedef struct {
     int32_t *free_count;       /* 1 */
 } sdlm_kv;
 
-/* The cache of a context, to work on it with the operators below in the stream order of the context: lengths are its c.  The memory stays the context's; pages belong to its own calls. */
+/* The cache of a context, to work on it with the operators below in the stream order of the context: lengths are its c.  The memory stays the context's; its
+ * pages too, which its own calls hand out: n_pages is 0 and what sdlm_kv_fork needs is NULL, so that it refuses the cache (a context is forked by sdlm_fork). */
 int sdlm_kv_describe(sdlm_ctx *ctx, sdlm_kv *kv);
 
 /*

@@ -1032,6 +1032,9 @@ int sdlm_kv_describe(sdlm_ctx *c, sdlm_kv *kv)
 {
     if (!c || !kv) return SDLM_EINVAL;
     *kv = cache_of(c, c->st.c);
+    // Which pages are free is the context's to know (its commits take pages off the list by a count of their own), and its lengths, pending tokens and batch go with a fork.
+    kv->n_pages = 0;
+    kv->backed = kv->page_refs = kv->free_pages = kv->free_count = nullptr;
     return SDLM_OK;
 }
 

@@ -493,6 +493,26 @@ def test_tree_behind_a_callers_graph_that_fills_the_context():
     ctx.close()
 
 
+def test_described_cache_is_not_forked():
+    """Pages are handed out by the context's own calls: the fork on the caller's tensors refuses them, before and behind a commit that takes some."""
+    import ctypes as C
+    ctx, om, m, tol, hist = setup("fp32", [16, 7], 4)
+    for _ in range(2):
+        desc = sdlm.KvDesc()
+        assert ctx.L.sdlm_kv_describe(ctx.h, C.byref(desc)) == 0
+        assert desc.n_pages == 0 and not (desc.backed or desc.page_refs or desc.free_pages or desc.free_count)
+        assert ctx.L.sdlm_kv_fork_workspace_bytes(C.byref(desc)) == 0
+        some = torch.zeros(1 << 20, dtype=torch.int32, device="cuda")
+        assert ctx.L.sdlm_kv_fork(C.byref(desc), some.data_ptr(), 2, 1, some.data_ptr(), some.data_ptr(), 4 << 20, None) == sdlm.EINVAL
+        assert "n_pages" in ctx.L.sdlm_op_error().decode()
+        check_history(ctx, om, m, tol, hist)
+        commit(ctx, hist, [[1, 2, 3, 4]] * 2, [2, 1])
+    ctx.fork([1, 0, 1])
+    hist = [list(hist[p]) for p in (1, 0, 1)]
+    check_history(ctx, om, m, tol, hist)
+    ctx.close()
+
+
 def test_described_cache_serves_the_operators():
     """Attention over a context's own cache through sdlm_kv_describe: a node that sees only the cache is a query over it."""
     import ctypes as C
