@@ -150,6 +150,21 @@ def test_forked_sequences_go_their_own_ways(kind, paged):
     ctx.close()
 
 
+@pytest.mark.parametrize("paged", [True, False])
+def test_forks_of_a_large_context(paged):
+    """64 sequences of up to 8192 tokens: a table of 32768 pages, more than one workgroup plans."""
+    D = 4
+    ctx, om, m, tol, hist = setup("fp32", [37, 16, 300], D, paged=paged, max_batch=64, max_seq_len=8192, n_pages=120)
+    rng = np.random.default_rng(4)
+    for parents in ([0, 2, 1, 2, 2], [4, 4, 0, 1], [3, 1, 0, 0, 2, 2, 1]):
+        ctx.fork(parents)
+        hist = [list(hist[p]) for p in parents]
+        check_history(ctx, om, m, tol, hist)
+        commit(ctx, hist, rng.integers(0, m.vocab, (len(parents), D)).tolist(), rng.integers(1, D + 1, len(parents)).tolist())
+    check_history(ctx, om, m, tol, hist)
+    ctx.close()
+
+
 def test_fork_shares_pages_and_frees_them():
     """Six samples of a prompt of 100 tokens in a pool of 20 pages: unshared they would need 42; then again and again without a leak."""
     ctx, om, m, tol, hist = setup("fp32", [100], 4, n_pages=20)

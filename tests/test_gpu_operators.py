@@ -590,6 +590,106 @@ def test_fork_refused_changes_nothing(parent, code, kw):
     assert np.array_equal(pool.float().cpu().numpy(), c["pool"])
 
 
+def large_case(seed, pages=2600, S=70, long=4700):
+    """A table of more entries than one workgroup holds (20480): a sequence of several hundred pages, short and empty ones, pages backed ahead, pages held in common with sequences in front."""
+    rng = np.random.default_rng(seed)
+    lens = [int(v) for v in rng.choice([0, 1, 15, 16, 17, 160, 500], S)]
+    lens[3], lens[40], lens[41], lens[66] = long, 4096, 333, 40
+    ahead = [int(v) for v in rng.choice([0, 0, 1, 2], S)]
+    c = cache_case(seed, lens, ahead, pages, layers=2, heads=(1, 32), shared={40: (3, 200), 41: (3, 20), 66: (41, 2)})
+    assert c["table"].size > 20480
+    return c, rng
+
+
+@pytest.mark.parametrize("share,pages", [(True, 2600), (False, 9000), (True, 12300)])
+@pytest.mark.parametrize("heirs", ["stay", "move", "none"])
+def test_fork_of_large_tables(heirs, share, pages):
+    """What more than one workgroup plans: parents that stay, that end and leave their pages to the first of their children, sequences without one, pages shared before, more than 256 pages a sequence."""
+    c, rng = large_case(20, pages)
+    S = len(c["lens"])
+    parent = rng.integers(-1, S, S)
+    parent[[3, 5, 9, 40, 69]] = {"stay": [3, 3, 40, 40, 3], "move": [40, 3, 3, 66, 41], "none": [-1, 1, 2, -1, 0]}[heirs]
+    if heirs == "none":
+        parent[np.isin(parent, [3, 40])] = 66
+    kv, pool, t = kv_of(c)
+    kv.fork(dev(parent), share=share)
+    kv.check()
+    want = plain.fork(c, [int(p) for p in parent], share)
+    assert not isinstance(want, int)
+    same_cache(want, pool, t)
+
+
+@pytest.mark.parametrize("n_new", [0, 1, 37])
+def test_fork_of_large_tables_to_fewer(n_new):
+    c, rng = large_case(21)
+    parent = [int(v) for v in rng.integers(0, 70, n_new)]
+    kv, pool, t = kv_of(c)
+    kv.fork(dev(np.array(parent, np.int32)))
+    kv.check()
+    same_cache(plain.fork(c, parent, True), pool, t)
+
+
+def test_fork_of_large_tables_again_and_again():
+    c, rng = large_case(22)
+    kv, pool, t = kv_of(c)
+    for step in range(6):
+        parent = [int(v) for v in rng.integers(0, 70, 70)]
+        if step == 0:
+            parent[:4] = [3, 3, 40, 3]
+        want = plain.fork(c, parent, True)
+        assert not isinstance(want, int)
+        kv.fork(dev(parent))
+        kv.check()
+        same_cache(want, pool, t)
+        c = {**want, "dtype": c["dtype"]}
+
+
+@pytest.mark.parametrize("bad,code", [("room", sdlm.ECAPACITY), ("parent", sdlm.EINVAL), ("below", sdlm.EINVAL), ("page", sdlm.EINVAL), ("no page", sdlm.EINVAL), ("both", sdlm.EINVAL)])
+def test_fork_of_large_tables_refused_changes_nothing(bad, code):
+    c, rng = large_case(23)
+    parent = np.arange(70)
+    if bad in ("room", "both"):
+        parent[:20] = 3                     # 20 copies of 294 pages
+    if bad in ("parent", "both"):
+        parent[69] = 70
+    if bad == "below":
+        parent[0] = -2
+    if bad in ("page", "no page"):
+        c["table"][3, 290] = {"page": 2600, "no page": -1}[bad]
+    kv, pool, t = kv_of(c)
+    kv.fork(dev(parent), share=False)
+    with pytest.raises(sdlm.SdlmError) as e:
+        kv.check()
+    assert e.value.code == code
+    for name, key in (("page_table", "table"), ("lengths", "lens"), ("backed", "held"), ("page_refs", "refs")):
+        assert np.array_equal(t[name].cpu().numpy(), c[key])
+    assert (t["free_pages"] == 99).all() and t["free_count"].item() == 99
+    assert np.array_equal(pool.float().cpu().numpy(), c["pool"])
+
+
+def test_a_captured_fork_of_a_large_table():
+    """Its launches in a graph, replayed on a cache that changes in between, with eager calls between the replays."""
+    c, rng = large_case(24)
+    kv, pool, t = kv_of(c)
+    parent = dev(np.arange(70))
+    start = [x.clone() for x in (pool, *t.values())]
+    kv.fork(parent)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kv.fork(parent)
+    for _ in range(3):
+        p = [int(v) for v in rng.integers(-1, 70, 70)]
+        for x, v in zip((pool, *t.values()), start):
+            x.copy_(v)
+        parent.copy_(dev(p))
+        g.replay()
+        kv.check()
+        want = plain.fork(c, p, True)
+        assert not isinstance(want, int)
+        same_cache(want, pool, t)
+
+
 # ---------------------------------------------------------------------------------------------------------------- compacting
 
 @pytest.mark.parametrize("dtype,heads,layers", [("bf16", (2, 64), 3), ("fp32", (1, 32), 1), ("fp32", (2, 128), 2), ("bf16", (3, 96), 2), ("bf16", (4, 128), 1)])
