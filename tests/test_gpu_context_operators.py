@@ -284,6 +284,32 @@ def test_verified_trees(kind, D, T, paged):
     ctx.close()
 
 
+@pytest.mark.parametrize("hidden", [256, 3200])      # down by split sums; by whole ones, which carry the norm across the layers
+@pytest.mark.parametrize("D,T", [(1, 16), (1, 1), (2, 5), (4, 3)])
+def test_trees_of_one_bf16_sequence(D, T, hidden, monkeypatch):
+    """At most 16 rows: the kernels of few rows, whose sums of squares lie where the attention's partial results do."""
+    monkeypatch.setitem(MODELS, "few", (syn.ModelCfg(3, hidden, 6, 2, 128, 512, 1000, dtype="bf16"), 0.05 if hidden < 1000 else 0.02, 2e-2))
+    ctx, om, m, tol, hist = setup("few", [600], D, max_batch=1, max_seq_len=700)
+    assert T * (D + 1 if D > 1 else 1) <= 16
+    rng = np.random.default_rng(D)
+    for step in range(2):
+        st = check_history(ctx, om, m, tol, hist)
+        tokens, parents = grow(ctx, m, st, 1, T, rng)
+        z = torch.full((1, T, m.vocab), float("nan"), device="cuda")
+        path, count, nxt = [torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((1, T), (1,), (1,))]
+        ctx.verify_tree(torch.from_numpy(tokens).cuda(), torch.from_numpy(parents).cuda(), path, count, nxt, z)
+        g = z.cpu().numpy()
+        for i in range(T):
+            ref = node_logits(om, hist[0], tokens[0], parents[0], i, D)
+            assert np.max(np.abs(g[0, i] - ref)) / np.max(np.abs(ref)) <= tol, (step, i)
+        want, y = walk(st.ids[0, 0].item(), tokens[0], parents[0], g[0].argmax(1))
+        assert len(want) >= 1 and path[0].tolist() == want + [-1] * (T - len(want)) and count.item() == len(want) and nxt.item() == y
+        ctx.tree_commit()
+        hist[0] += [int(tokens[0, i]) for i in want] + [y]
+    check_history(ctx, om, m, tol, hist)
+    ctx.close()
+
+
 @pytest.mark.parametrize("heads,d", [(160, 128), (600, 32)])
 def test_trees_of_many_kv_heads(heads, d, monkeypatch):
     """More kv heads than 8 MB of partial results hold, and more rows than the small launch takes."""
