@@ -356,13 +356,13 @@ const char *sdlm_op_error(void);
  *   - w >= min_p (min_p <= 0 or NaN: all; above 1: none);
  * the first is always kept.  Drawn is the first kept token, in that order, whose running weight exceeds u times the weight of all kept ones.  A temperature <= 0 (or NaN)
  * draws the first.  Where the largest logit is +infinity, only the tokens with it have weight.  A row without any token above -infinity gives id -1 and probability 0.
- * Weights are held to 2^-45 of the largest, and where the whole row counts (no top_k) to 2^-30 of themselves, in integers, equal ones for equal logits: a result does not depend on the launch or on the row's neighbours.  A token whose weight is below that is not drawn.
+ * Weights are held to 2^-45 of the largest, where the whole row counts (no top_k) to 2^-44 of it and 2^-29 of themselves, in integers, equal ones for equal logits: a result does not depend on the launch or on the row's neighbours.  A token whose weight is below that is not drawn.
  */
 typedef struct {
     const void *logits;        /* [dev] rows x vocab, element type `dtype` */
     int64_t row_stride;        /* elements between rows, >= vocab */
     int32_t dtype;             /* 0: fp32, 1: bf16 */
-    int32_t rows, vocab;       /* rows 0 .. 1048576, rows * ((vocab + 7) / 16384 + 1) at most 2^24; vocab 1 .. 524288 */
+    int32_t rows, vocab;       /* rows 0 .. 1048576, vocab 1 .. 524288, rows * ceil((vocab + 7) / 16384) below 2^24 */
     const float *temperature;  /* [dev, rows] or NULL: 1 */
     const int32_t *top_k;      /* [dev, rows] or NULL: off */
     const float *top_p, *min_p;/* [dev, rows] or NULL: off */

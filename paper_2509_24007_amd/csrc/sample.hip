@@ -2,7 +2,7 @@
 //
 // The tokens of a row are ordered by logit, equal ones by index.  All filters keep a first part of that order, and the uniform number picks from the kept part
 // in that order.  Weights are integers in units of 2^-44 of the largest (or of the power of two above it): their sums do not depend on the order of the threads, and
-// their error (2^-45 of the largest a token, and 2^-30 of itself where the histogram counts) is far below the weight of any token that a draw could fall on.
+// their error (2^-45 of the largest a token; 2^-44 of it and 2^-29 of itself where the histogram counts) is far below the weight of any token that a draw could fall on.
 //
 // Two launches.  The first reads the logits once, all units together: a thread takes 64 of them and leaves the maxima of its runs, and for a row whose filters need the
 // weight of the whole row (no top-k) a workgroup also leaves a histogram of the weights over 1/32 octaves.  The second has a workgroup a row, which sorts only what matters:
@@ -297,7 +297,8 @@ __device__ inline double exponent(float z, double cs)
     return y;
 }
 
-// 2^d in units of 2^-44, d <= 0: a table of 2^(j / 64) and a cubic for the rest, to 30 bits, which depend on d's fraction alone.  So equal logits have equal weights whatever power of two they
+// 2^d in units of 2^-44, d <= 0: a table of 2^(j / 64) and a cubic for the rest, which depend on d's fraction alone.  The cubic's four fp32
+// roundings are 2^-24 of |r| <= ln 2 / 128 each, its remainder r^4 / 24 and the result's last bit 2^-31: together below 2^-29 (largest found over 4e7 values: 2^-29.5).  So equal logits have equal weights whatever power of two they
 // are held against, in both launches, and sums of weights down to 2^-14 of the largest are exact: a bound that falls between equal logits falls between the same ones as in the definition.
 __device__ inline u64 fast_weight(double d, const double *table)
 {

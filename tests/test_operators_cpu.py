@@ -133,6 +133,13 @@ def test_sizes_beyond_a_launch_are_refused():
     assert L.sdlm_tree_attention_workspace_bytes(C.byref(kv(max_seqs=1 << 20, pages_per_seq=1)), 4, 1 << 20, 1024, 0) == 0
 
 
+def test_largest_sample():
+    """rows * ceil((vocab + 7) / 16384) below 2^24, as the header says."""
+    need = sdlm.load().sdlm_sample_workspace_bytes
+    assert need(1 << 20, 15 * 16384 - 7) > 0 and need(1 << 20, 15 * 16384 - 6) == 0
+    assert need(508400, 1 << 19) > 0 and need(508401, 1 << 19) == 0      # 33 pieces a row
+
+
 def test_struct_sizes_agree_with_the_header():
     """Sizes of the argument structs as a C compiler lays them out on this ABI."""
     assert C.sizeof(sdlm.SampleArgs) == 88 and C.sizeof(sdlm.KvDesc) == 96 and C.sizeof(sdlm.TreeArgs) == 96
