@@ -9,13 +9,16 @@
 //   - top-k: the k-th largest of the runs' maxima is no more than the k-th largest logit, so the candidates are what reaches it, in the few runs that do;
 //   - min-p: the candidates are what reaches min_p of the largest;
 //   - otherwise the histogram says in which bin the weight passes top_p, and in which bin the draw falls, and the candidates are that bin.
-// Where a row has too few runs for its top-k, the k-th logit itself is searched by digits.  Where the candidates do not fit (thousands of equal logits, top-k beyond CAND), or where the exponents leave the histogram's range, the row is searched by digits
-// of the logits' order-preserving integers instead, without sorting, in a dozen passes.
+// Where a row has too few runs for its top-k, the k-th logit itself is searched by digits.  Where more than CAND candidates come together, or where the exponents leave the histogram's range, the row is searched by digits
+// of the logits' order-preserving integers instead, without sorting, in a dozen passes.  Those are: top-k beyond CAND; thousands of equal logits; a min-p that more than CAND tokens reach; and without top-k
+// or min-p rows so flat that a bin, which is 0.0217 t wide in logits, holds more than CAND: one of V logits that fall off as e^(-z / s) does where 0.0217 V t / s is above CAND (152064 and s = 1.1: t = 1.4), and with an
+// infinite temperature any with more than CAND logits.
 //
-// us: one row of 151936 fp32 5 + 13, 256 rows of 152064 with mixed settings 51 + 46, 33 rows of 33003 bf16 13 + 28.  The first launch is bound by the read where no row asks for weights (256 rows 39, 4.0 TB/s),
+// us: one row of 151936 fp32 5 + 13, 256 rows of 152064 with mixed settings 52 + 46, 33 rows of 33003 bf16 13 + 28.  The first launch is bound by the read where no row asks for weights (256 rows 39, 4.0 TB/s),
 // else by the weights' instructions.  The second is a chain of scans and synchronisations in one workgroup, whose longest part, where a bound lies far down a flat tail, is the read of the whole row (about
-// 25 each time, by its instructions).  256 rows with top_k = 2048 86, 4000 (the k-th by digits) 368, 5000 (all by digits) 760; 36 rows of 7452 bf16 with
-// top_k = 1000, which have fewer runs than that, 66 (by digits 108).
+// 25 each time, by its instructions).  256 rows with top_k = 2048 76, 4000 (the k-th by digits) 340, 5000 (all by digits) 732; 36 rows of 7452 bf16 with
+// top_k = 1000, which have fewer runs than that, 66 (by digits 108).  Flat rows (256 of 152064, s = 1.1) with top-p 0.99: t = 1.3 159, from 1.5 on 783 (by digits); without top-p 117, 417 to 556; one row with
+// top-p 85, 520.
 #include "ops.hpp"
 
 namespace sdlm {

@@ -125,8 +125,9 @@ __global__ __launch_bounds__(256) void tree_rows_k(TreeArgs a)
 // dealt out to them in equal runs: no unit waits for another at the end, whatever the lengths are.  A workgroup's run may end inside a block; such a part leaves a
 // maximum, a sum and an unnormalised output, and the parts of a block are merged by a second launch.  At most its first and its last part are incomplete, so a
 // workgroup has two places for them.  fp32 tiles and operands take the instruction of 16 x 16 x 4, whose operands are neighbours in the tiles as they are.
-// us, attention and merge: 64 sequences of 2048 to 4096 positions, up to 16 nodes, 28 / 4 heads 100 + 11 (413 MB, bound by the cache);  4 of up to 8192, up to 256 nodes, 16 / 2 heads 85 + 8 (480 TFLOP/s, bound by
-// the vector instructions between the two products);  one of 512, 12 nodes 8 + 6, a chain of round trips.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
+// us, attention and merge, averages under the profiler (a call among others): 64 sequences of 2048 to 4096 positions, up to 16 nodes, 28 / 4 heads 112 + 11 (112: 413 MB, 3.7 TB/s);  4 of up to 8192, up to 256
+// nodes, 16 / 2 heads 114 + 9 (103: 41 GFLOP, 400 TFLOP/s);  one of 512, 12 nodes 10 + 6 (16), a chain of round trips.  The wide trees' units are at the matrix instructions for 38 % of their time, at the vector
+// instructions between the two products for 45 % and at LDS for 26 %, with two wavefronts a SIMD to overlap them.  The runs follow from the lengths by prefix sums over the sequences, a lane a sequence, that every wavefront makes for itself.
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
@@ -617,13 +618,13 @@ __global__ __launch_bounds__(256) void tree_merge_k(MfmaArgs a)
 }
 
 // Queries of a wavefront in units of 16: by the most queries that a kv head has in a sequence.  One for up to 64, so that all four wavefronts have some; beyond, two, which reads
-// every tile half as often from memory and LDS.  us, one / two: 64 sequences of 3000 positions, 7 queries 84 / 87, 56 queries 100 / 104, up to 112 queries 132 / 110;  4 trees of 1200 to
-// 2048 queries over 6144 positions 116 / 98.  Three would need more registers than two workgroups a unit leave (98 -> 122).
+// every tile half as often from memory and LDS.  us, one / two: 64 sequences of 3000 positions, 7 queries 84 / 88, 56 queries 98 / 105, 70 queries 113 / 111, 112 queries 126 / 124;  4 trees of 1200 to
+// 2048 queries over 6144 positions 120 / 103.  Three would need more registers than two workgroups a unit leave.
 int query_tiles(int queries) { return queries <= 64 ? 1 : 2; }
 
 // fp32 calls that one launch of tree_rows_k serves faster: by the length of the longest prefix as the caller names it or what the table holds (a wrong one costs time, nothing else), and the
-// keys that all rows read together.  us, rows / matrix cores: 1 sequence of 300 positions, 8 nodes, 4 heads 14.8 / 17.4;  500 positions, 12 nodes, 12 heads 14.6 / 21.0;  3 of 700, 30 nodes,
-// 6 heads 14.4 / 19.7;  beyond: 1 of 4000, 12 nodes, 12 heads 71.7 / 42.9;  4 of 1000, 16 nodes, 28 heads 84.4 / 34.5;  4 of 4000, 128 nodes, 40 heads 8305 / 388 (108 TFLOP/s).
+// keys that all rows read together.  us, rows / matrix cores: 1 sequence of 300 positions, 8 nodes, 4 heads 14.2 / 16.8;  500 positions, 12 nodes, 12 heads 14.6 / 20.7;  3 of 700, 30 nodes,
+// 6 heads 14.2 / 19.9;  beyond: 1 of 4000, 12 nodes, 12 heads 71.7 / 42.9;  4 of 1000, 16 nodes, 28 heads 84.4 / 34.5;  4 of 4000, 128 nodes, 40 heads 8305 / 386 (109 TFLOP/s of the 154 that a library's fp32 product reaches here).
 bool few_rows(const sdlm_kv &kv, const sdlm_tree_args &t)
 {
     const double len = t.max_len ? t.max_len : (double)kv.pages_per_seq * PAGE;
